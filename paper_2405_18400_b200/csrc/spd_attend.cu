@@ -25,8 +25,8 @@ template <int MODE> void tuning(int d, int *warps, int *per_sm) {
 }
 
 // Microseconds of a step among others, 128 dimensions: of a prefix tile of 16, 32 and 64 (of few) rows by a block, of an own tile by a warp; by mode.
-constexpr float kStepCost[6][3] = {{1.5f, 1.95f, 2.8f}, {2.1f, 3.5f, 6.2f}, {2.7f, 3.8f, 6.4f}, {2.4f}, {2.5f}, {2.6f}};
-constexpr float kOwnStepCost[6] = {1.7f, 2.2f, 2.7f, 3.2f, 3.4f, 3.4f};
+constexpr float kStepCost[6][3] = {{1.55f, 2.2f, 3.5f}, {2.1f, 3.5f, 6.2f}, {2.7f, 3.8f, 6.4f}, {2.4f}, {2.5f}, {2.6f}};
+constexpr float kOwnStepCost[6] = {1.8f, 2.2f, 2.7f, 3.2f, 3.4f, 3.4f};
 
 struct AttendPlan {
   int rt, many_parts, blocks, warps, rows_o, device;

@@ -28,8 +28,9 @@
 // copy's 6.46); 8 rows behind 4 x 4096 positions of 32 heads 50 us for 268 MB; 64 requests behind 2048 positions with 50 to 200 of their own 44 us for 165 MB;
 // three float32 rows behind 2048 positions 14.6 us for 34 MB, eight times as many 51 for 266; 31 float32 rows over 1001 positions of a float32 cache, 40 heads, 33 us for 52 MB.
 //
-// Roundings.  bf16 queries and cache: products exact, sums float32, the softmax weights e^(s-m) <= 1 rounded to bf16 as the second
-// product's operand (2^-9 each, as the output's own rounding) while their sum is taken before rounding.  float32 queries with a
+// Roundings.  bf16 queries and cache: products exact, sums float32, the softmax weights e^(s-m) <= 1 as two bf16 terms (the first by truncation, exact; the
+// second to 2^-16 of the weight), so that the output's own rounding is all that shows (error 1.66e-3, as float32 arithmetic rounded once; with weights
+// of one term, 2^-9 each, it was 2.21e-3.  The second term's products cost 64 requests 4 us of 53 and four long prompts 2 of 74, caches cold.)  float32 queries with a
 // bf16 cache: queries and weights as three exact bf16 terms.  float32 cache: both sides of both products as two tf32 terms (11 + 11
 // bits), three products.
 #pragma once
@@ -240,6 +241,12 @@ __device__ __forceinline__ void split_terms(float x, float y, uint32_t *t) {
     x -= __uint_as_float(bx & 0xffff0000u);
     y -= __uint_as_float(by & 0xffff0000u);
   }
+}
+// A pair of values as two bf16 terms, packed: the first by truncation (exact), what it leaves to the nearest.  The rest is 2^-16 of a value at most.
+__device__ __forceinline__ void split_weights(float x, float y, uint32_t &high, uint32_t &low) {
+  const uint32_t bx = __float_as_uint(x), by = __float_as_uint(y);
+  high = __byte_perm(bx, by, 0x7632);
+  low = pack_bf16(x - __uint_as_float(bx & 0xffff0000u), y - __uint_as_float(by & 0xffff0000u));
 }
 
 // ---- one tile's piece
@@ -842,7 +849,7 @@ struct Attending {
             for (int c = 0; c < 4; ++c) o[r][4 * jj + i][c] = fmaf(o[r][4 * jj + i][c], f[r][c >> 1], sum[r][i][c]);
       }
     } else {
-      constexpr int kTerms = MODE == kAttTerms ? 3 : kEight ? 2 : 1;
+      constexpr int kTerms = MODE == kAttTerms ? 3 : kEight || MODE == kAttBf16 ? 2 : 1;
       uint32_t w[NT][kTerms][4];
       if constexpr (kFew) {
 #pragma unroll
@@ -863,7 +870,7 @@ struct Attending {
         for (int j = 0; j < 4; ++j) {  // rows g, g + 8 of positions 2t, then of 2t + 8
           const float x = s[0][2 * n + (j >> 1)][2 * (j & 1)], y = s[0][2 * n + (j >> 1)][2 * (j & 1) + 1];
           if constexpr (MODE == kAttBf16) {
-            w[n][0][j] = pack_bf16(x, y);
+            split_weights(x, y, w[n][0][j], w[n][kTerms - 1][j]);
           } else {
             uint32_t term[3];
             split_terms(x, y, term);
