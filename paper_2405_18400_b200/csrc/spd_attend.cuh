@@ -189,13 +189,14 @@ __device__ __forceinline__ Split split_blocks(int blocks, int warps, const Weigh
   return {n, rest < own.steps ? rest : own.steps};
 }
 // Run i of n over `steps` begins at step floor(i steps / n): all runs alike but for one step, and whole numbers of them to tiles that
-// are alike.  run_of: the run that has a step.  (In 64 bits only where 32 do not hold the product of up to 2048 runs.)
-static __device__ __noinline__ int wide_ratio(unsigned a, unsigned b, unsigned minus, unsigned by) { return (int)(((unsigned long long)a * b - minus) / by); }
-__device__ __forceinline__ int run_start(int i, int n, int steps) {
-  return steps < 1 << 21 ? (int)((unsigned)i * (unsigned)steps / (unsigned)n) : wide_ratio(i, steps, 0, n);
+// are alike.  run_of: the run that has a step.  (In 64 bits only where 32 do not hold n steps, which no product here passes.)
+static __host__ __device__ __noinline__ int wide_ratio(unsigned a, unsigned b, unsigned minus, unsigned by) { return (int)(((unsigned long long)a * b - minus) / by); }
+__host__ __device__ __forceinline__ bool wide(int n, int steps) { return ((unsigned long long)(unsigned)n * (unsigned)steps) >> 32 != 0; }
+__host__ __device__ __forceinline__ int run_start(int i, int n, int steps) {
+  return !wide(n, steps) ? (int)((unsigned)i * (unsigned)steps / (unsigned)n) : wide_ratio(i, steps, 0, n);
 }
-__device__ __forceinline__ int run_of(int step, int n, int steps) {
-  return steps < 1 << 21 ? (int)((((unsigned)step + 1) * (unsigned)n - 1) / (unsigned)steps) : wide_ratio(step + 1, n, 1, steps);
+__host__ __device__ __forceinline__ int run_of(int step, int n, int steps) {
+  return !wide(n, steps) ? (int)((((unsigned)step + 1) * (unsigned)n - 1) / (unsigned)steps) : wide_ratio(step + 1, n, 1, steps);
 }
 
 // ---- instructions
