@@ -421,8 +421,8 @@ int spd_shared_attention_bytes(const spd_attention_args *args, size_t *bytes);
  * Where fewer options than beams exist, the rest gets token -1, parent = its own number, score minus infinity, length 0, not ended.
  * The rank is decided in 64 bits.  1 <= beams <= 32, vocab <= 262144.  length and ended may be NULL (zeros), new_length and
  * new_ended too; they are [requests][beams] and contiguous, as score and new_*, which must not overlap what is read.  workspace: spd_beam_select_bytes of DEVICE
- * memory, 256-byte aligned, zeroed once before its first use (calls leave its counters at zero) and not shared by
- * calls that overlap.
+ * memory, 256-byte aligned, zeroed once before its first use (calls leave its counters at zero, and no call's data lies where
+ * another's counters do) and not shared by calls that overlap.  It serves calls of as many requests or fewer, and whatever else needs no more bytes.
  */
 typedef struct {
   const void *logits;

@@ -83,7 +83,7 @@ def spd_shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
 
 
 def spd_beam_select_workspace(logits: torch.Tensor) -> torch.Tensor:
-    """Workspace for selections of this shape and type; to be kept between calls (it comes zeroed, and calls leave it so)."""
+    """Workspace for selections of this shape and type, or of fewer requests; to be kept between calls (its counters come zeroed, and calls leave them so)."""
     return torch.zeros((_tensors or load_tensors()).beam_select_bytes(logits), dtype=torch.uint8, device=logits.device)
 
 

@@ -24,6 +24,9 @@ constexpr int kSelGroups = kSelThreads / 4;
 constexpr int kSelMaxBeams = 32;
 constexpr int kSelMaxSlices = 32;   // a lane each when their sums are joined
 constexpr int kSelMaxVocab = 262144;
+constexpr int kSelMaxRequests = 65535;
+// The counters have their place to themselves whatever the call's sizes are, so that a workspace may serve calls of different sizes in turn.
+constexpr size_t kSelCounters = ((size_t)kSelMaxRequests * 4 + 255) / 256 * 256;
 constexpr int kSelJoinBytes = 44 * 1024;
 
 struct Select {
@@ -430,34 +433,50 @@ __global__ void __launch_bounds__(kSelThreads) spd_select_kernel(const __grid_co
 // Vectors of 16 bytes a thread takes: what gives the fullest SM the least to do, a block being worth some 6 logits a thread beside its own
 // (16 x 8 beams of 32000: 13.4 us in 256 blocks, 14.3 in 512, 14.9 in 1024; 32 x 3 beams of as many, bf16: 11.8 in 192, 10.3 in 384, 11.2 in 768); but
 // no more lists than a request's last block merges quickly (64): 16 beams of one request in 512 lists took 73 us, in 64 12.
+int64_t slices_of(int nv, int vocab, int per_vector, int skew) {
+  const int64_t slice = (int64_t)kSelThreads * nv * per_vector;
+  return (vocab + skew + slice - 1) / slice;
+}
+bool few_lists(int64_t slices, int beams) { return slices <= kSelMaxSlices && slices * beams <= 64; }
 int vectors(int64_t rows, int beams, int vocab, int per_vector, int skew) {
   int best = 64 / per_vector;
   int64_t least = INT64_MAX;
   for (int nv = best; nv >= 1; nv /= 2) {
-    const int64_t slice = (int64_t)kSelThreads * nv * per_vector, slices = (vocab + skew + slice - 1) / slice;
+    const int64_t slices = slices_of(nv, vocab, per_vector, skew);
     const int64_t work = (rows * slices + 147) / 148 * (nv * per_vector + 6);
-    if (slices > kSelMaxSlices || slices * beams > 64 || work >= least) continue;
+    if (!few_lists(slices, beams) || work >= least) continue;
     least = work;
     best = nv;
   }
   return best;
 }
+// The most slices that any number of requests is given.
+int64_t most_slices(int beams, int vocab, int per_vector, int skew) {
+  int64_t most = slices_of(64 / per_vector, vocab, per_vector, skew);
+  for (int nv = 64 / per_vector; nv >= 1; nv /= 2) {
+    const int64_t slices = slices_of(nv, vocab, per_vector, skew);
+    if (few_lists(slices, beams) && slices > most) most = slices;
+  }
+  return most;
+}
 struct SelectPlan {
   int nv, slices, keys_fit;
   size_t stats, keys, per, bytes, smem;
 };
+void select_layout(SelectPlan *l, int64_t rows, int beams, int64_t slices) {
+  l->stats = kSelCounters;
+  l->keys = l->stats + ((size_t)rows * slices * 8 + 255) / 256 * 256;
+  l->per = l->keys + ((size_t)rows * slices * beams * 8 + 255) / 256 * 256;
+  l->bytes = l->per + (size_t)rows * 16;
+}
 SelectPlan select_plan(const spd_select_args &a, bool on_vectors) {
   SelectPlan l;
   const int per = 16 / (int)type_bytes(a.x_dtype);
   const int skew = on_vectors ? 0 : per - 1;
   const int64_t rows = (int64_t)a.requests * a.beams;
   l.nv = vectors(rows, a.beams, a.vocab, per, skew);
-  const int slice = kSelThreads * l.nv * per;
-  l.slices = (a.vocab + skew + slice - 1) / slice;
-  l.stats = ((size_t)a.requests * 4 + 255) / 256 * 256;
-  l.keys = l.stats + ((size_t)rows * l.slices * 8 + 255) / 256 * 256;
-  l.per = l.keys + ((size_t)rows * l.slices * a.beams * 8 + 255) / 256 * 256;
-  l.bytes = l.per + (size_t)rows * 16;
+  l.slices = (int)slices_of(l.nv, a.vocab, per, skew);
+  select_layout(&l, rows, a.beams, l.slices);
   const size_t slice_list = (size_t)a.beams * l.nv * per * 8;
   size_t join = (size_t)a.beams * a.beams * (sizeof(Option) + 8);
   const size_t lists = (size_t)a.beams * l.slices * a.beams * 8;
@@ -487,7 +506,7 @@ int select_launch(const Select &p, const SelectPlan &l) {
 
 int select_check(const spd_select_args *a) {
   if (!a || a->requests < 0 || a->beams < 1 || a->vocab < 1 || !known_type(a->x_dtype)) return SPD_EINVAL;
-  if (a->beams > kSelMaxBeams || a->vocab > kSelMaxVocab || a->requests > 65535) return SPD_ERANGE;
+  if (a->beams > kSelMaxBeams || a->vocab > kSelMaxVocab || a->requests > kSelMaxRequests) return SPD_ERANGE;
   return SPD_OK;
 }
 
@@ -498,12 +517,11 @@ extern "C" int spd_beam_select_bytes(const spd_select_args *args, size_t *bytes)
   using namespace spd;
   const int rc = select_check(args);
   if (rc || !bytes) return rc ? rc : SPD_EINVAL;
-  // Rows that begin on a vector may be cut into other slices than rows that do not: the larger need of the two.
-  *bytes = 0;
-  for (int on_vectors = 0; on_vectors < 2; ++on_vectors) {
-    const size_t need = select_plan(*args, on_vectors != 0).bytes;
-    if (need > *bytes) *bytes = need;
-  }
+  // The most that these requests or fewer need, whether rows begin on a vector or not: the number of slices goes by both.
+  const int per = 16 / (int)type_bytes(args->x_dtype);
+  SelectPlan l;
+  select_layout(&l, (int64_t)args->requests * args->beams, args->beams, most_slices(args->beams, args->vocab, per, per - 1));
+  *bytes = l.bytes;
   return SPD_OK;
 }
 

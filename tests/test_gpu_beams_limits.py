@@ -28,3 +28,42 @@ def test_own_parts_of_millions_of_steps(kv, own):
         # float32 arithmetic in parts of a hundred steps: scores and sums to some 2^-21 (the sum's terms are of random sign), ten times that to spare
         assert (got[lo: lo + 64].double() - want).abs().max() < 2.0 ** -17
         assert (lse[lo: lo + 64].double() - want_lse).abs().max() < 2.0 ** -17
+
+
+# ---------------------------------------------------------------- selection: one workspace, calls of different sizes in turn
+def selection(seed, r, w, v, offset=0):
+    g = gen(seed)
+    wide = normal(g, r, w, v + 4)
+    return wide[..., offset: offset + v], -torch.rand(r, w, generator=g, device=DEV)
+
+
+def same_selections(z, score, workspace):
+    want = P.spd_beam_select(z, score)
+    got = P.spd_beam_select(z, score, workspace=workspace)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_selections_workspace_serves_other_numbers_of_requests():
+    z, score = selection(1, 100, 4, 3000)
+    ws = P.spd_beam_select_workspace(z)
+    for n in (100, 10, 100, 1, 65, 100):
+        same_selections(z[:n], score[:n], ws)
+    big = P.spd_beam_select_workspace(selection(2, 150, 16, 9000)[0])
+    for k, (r, w, v, offset) in enumerate([(150, 16, 9000, 0), (7, 5, 40000, 1), (150, 2, 300, 0), (3, 16, 9000, 2), (90, 8, 5000, 0), (150, 16, 9000, 3)]):
+        same_selections(*selection(10 + k, r, w, v, offset), big)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("w,v", [(3, 32000), (8, 32000), (2, 100000), (16, 4099), (32, 40000)])
+def test_a_selections_workspace_is_enough_for_fewer_requests(dtype, w, v):
+    """The fewer requests, the more slices a row is cut into; the room asked for covers that, for rows that begin on a vector and others."""
+    z, score = selection(3, 40, w, v)
+    z = z.to(dtype)
+    ws = P.spd_beam_select_workspace(z)
+    for n in (40, 39, 37, 36, 31, 19, 18, 12, 9, 5, 3, 2, 1):
+        assert P.spd_beam_select_workspace(z[:n]).numel() <= ws.numel()
+        same_selections(z[:n], score[:n], ws)
+        if v % 8:
+            continue
+        skewed = torch.empty(n, w, v + 1, dtype=dtype, device=DEV)[..., 1:].copy_(z[:n])
+        same_selections(skewed, score[:n], ws)
