@@ -391,7 +391,8 @@ int spd_cache_append(const spd_append_args *args);
  * their value or better for bf16 queries, 2^-22 for float32 ones; their sum is taken in float32.  head_dim a multiple of 8 (of 4 for a float32
  * cache), at most 256; cache rows of a head start on 16 bytes.  b <= 4096, n <= 2^24, slots < 2^31 (else SPD_ERANGE).  workspace: spd_shared_attention_bytes of DEVICE memory,
  * 256-byte aligned, not shared by calls that overlap; the counts n, b, g, heads and head_dim, the types of `args` and whether q_start is
- * set are all that function reads (set is the larger need).
+ * set are all that function reads (set is the larger need).  Calls with the same heads, head_dim and types and as many rows,
+ * sequences and prefixes or fewer need no more.
  */
 typedef struct {
   const void *q, *k_cache, *v_cache;

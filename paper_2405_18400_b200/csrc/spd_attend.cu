@@ -16,6 +16,12 @@ int mode_of(const spd_attention_args &a) {
   if (a.x_dtype == SPD_F32 && a.kv_dtype == SPD_F32) return rows <= 8 * groups ? kAttFewFloat : kAttFloat;
   return -1;
 }
+// Whether a call of these types and dimensions may go to a kernel, by its counts.
+bool serves(int mode, const spd_attention_args &a) {
+  if (a.x_dtype == SPD_BF16) return mode == kAttBf16;
+  if (a.kv_dtype == SPD_F32) return mode == kAttFloat || mode == kAttFewFloat;
+  return mode == kAttTerms || mode == kAttFew || (mode == kAttEight && a.head_dim <= 128);
+}
 template <int MODE> void tuning(int d, int *warps, int *per_sm) {
   if constexpr (MODE != kAttEight) {
     if (d > 128) *warps = AttendTune<MODE, 256>::nw, *per_sm = AttendTune<MODE, 256>::per_sm;
@@ -48,9 +54,8 @@ int attend_check(const spd_attention_args *a) {
   return SPD_OK;
 }
 
-int attend_plan(const spd_attention_args &a, AttendPlan *l) {
+int attend_plan(const spd_attention_args &a, int mode, AttendPlan *l) {
   int warps = 0, per_sm = 0, sms = 0;
-  const int mode = mode_of(a);
   if (mode == kAttBf16) tuning<kAttBf16>(a.head_dim, &warps, &per_sm);
   else if (mode == kAttTerms) tuning<kAttTerms>(a.head_dim, &warps, &per_sm);
   else if (mode == kAttFew) tuning<kAttFew>(a.head_dim, &warps, &per_sm);
@@ -84,8 +89,9 @@ int attend_plan(const spd_attention_args &a, AttendPlan *l) {
   l->rows_o = a.q_start || ratio > rows_of ? rows_of : (int)ratio;
   l->prefix_parts = a.g ? l->blocks + a.n_kv_heads * (rows / (rows_of * l->rt) + a.g) : 0;
   l->own_parts = (long long)l->blocks * warps + a.n_kv_heads * (rows / rows_of + a.b);
-  // (room for the highest tiles, so that the need does not hang on the tables)
-  const size_t part_rows = a.g ? 64 * ((size_t)l->blocks + a.n_kv_heads * (size_t)a.g) + (size_t)a.n_kv_heads * rows : 0;
+  // (room for the highest tiles that the kernel has, so that the need does not hang on the tables)
+  const size_t highest = rows_of < 16 ? rows_of : 64;
+  const size_t part_rows = a.g ? highest * ((size_t)l->blocks + a.n_kv_heads * (size_t)a.g) + (size_t)a.n_kv_heads * rows : 0;
   l->prefix_ml = up(part_rows * a.head_dim * 4);
   l->own_o = l->prefix_ml + up(part_rows * 8);
   l->own_ml = l->own_o + up((size_t)l->own_parts * l->rows_o * a.head_dim * 4);
@@ -100,9 +106,14 @@ extern "C" int spd_shared_attention_bytes(const spd_attention_args *args, size_t
   using namespace spd;
   int rc = attend_check(args);
   if (rc || !bytes) return rc ? rc : SPD_EINVAL;
-  AttendPlan l;
-  if ((rc = attend_plan(*args, &l))) return rc;
-  *bytes = l.bytes;
+  // Each kernel's need grows with the counts, but fewer rows or prefixes may go to another kernel: the most that one of these types needs.
+  *bytes = 0;
+  for (const int mode : {kAttBf16, kAttTerms, kAttFloat, kAttFew, kAttFewFloat, kAttEight}) {
+    AttendPlan l;
+    if (!serves(mode, *args)) continue;
+    if ((rc = attend_plan(*args, mode, &l))) return rc;
+    if (l.bytes > *bytes) *bytes = l.bytes;
+  }
   return SPD_OK;
 }
 
@@ -121,7 +132,7 @@ extern "C" int spd_shared_attention(const spd_attention_args *args) {
   if (a.b < 1 || (!a.q_start && a.n != a.b)) return SPD_EINVAL;
   if (a.slots > 0x7fffffff) return SPD_ERANGE;
   AttendPlan l;
-  if ((rc = attend_plan(a, &l))) return rc;
+  if ((rc = attend_plan(a, mode_of(a), &l))) return rc;
   if (a.workspace_bytes < (int64_t)l.bytes) return SPD_ENOMEM;
   // steps in 31 bits
   const int step = a.kv_dtype == SPD_F32 ? kPositions<kAttFloat> : kPositions<kAttBf16>;

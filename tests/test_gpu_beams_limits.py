@@ -67,3 +67,37 @@ def test_a_selections_workspace_is_enough_for_fewer_requests(dtype, w, v):
             continue
         skewed = torch.empty(n, w, v + 1, dtype=dtype, device=DEV)[..., 1:].copy_(z[:n])
         same_selections(skewed, score[:n], ws)
+
+
+# ---------------------------------------------------------------- attention: one workspace for as many rows, sequences and prefixes or fewer
+def attention_room(x, kv, heads, kv_heads, dim, n, b, g):
+    q, cache = torch.empty(n, heads, dim, dtype=x, device=DEV), torch.empty(1, kv_heads, dim, dtype=kv, device=DEV)
+    tables = torch.empty(b, 1, dtype=torch.int32, device=DEV)
+    return P.spd_shared_attention_workspace(q, cache, tables, tables[:g] if g else None).numel()
+
+
+@pytest.mark.parametrize("x,kv,heads,kv_heads,dim,more,fewer", [
+    (F32, BF16, 8, 8, 128, (8, 8, 1), (4, 4, 1)), (F32, F32, 8, 8, 128, (9, 9, 1), (8, 8, 1)), (F32, F32, 40, 40, 128, (16, 8, 1), (8, 8, 1)),
+    (F32, BF16, 1, 1, 128, (8, 8, 8), (8, 8, 1)), (F32, BF16, 1, 1, 128, (8, 8, 8), (8, 8, 0)), (F32, BF16, 32, 32, 64, (20, 20, 1), (4, 4, 1))])
+def test_an_attentions_workspace_is_enough_for_less(x, kv, heads, kv_heads, dim, more, fewer):
+    assert attention_room(x, kv, heads, kv_heads, dim, *more) >= attention_room(x, kv, heads, kv_heads, dim, *fewer)
+
+
+@pytest.mark.parametrize("x,kv", [(BF16, BF16), (F32, BF16), (F32, F32)])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 4, 64), (8, 2, 128), (6, 1, 256)])
+def test_smaller_calls_in_a_larger_ones_workspace(x, kv, heads, kv_heads, dim):
+    """A search whose beams and prompts end: fewer rows go to other kernels, with the room that was taken at its start."""
+    g = gen(dim)
+    groups, beams, prefix, own, slots = 3, 8, 150, 20, 900
+    b = groups * beams
+    kc, vc = normal(g, slots, kv_heads, dim).to(kv), normal(g, slots, kv_heads, dim).to(kv)
+    q = normal(g, b, heads, dim).to(x)
+    ptab = torch.randint(0, slots // 10, (groups, prefix // 10), generator=g, device=DEV).to(torch.int32)
+    otab = torch.randint(0, slots, (b, own), generator=g, device=DEV).to(torch.int32)
+    ws = P.spd_shared_attention_workspace(q, kc, otab, ptab)
+    for n in (groups, 2, 1, 0):
+        for w in (beams, 5, 4, 2, 1):
+            rows = max(n, 1) * w
+            kw = dict(prefix_table=ptab[:n], prefix_len=i32([prefix] * n), prefix_page=10, group_start=i32([w * i for i in range(n + 1)])) if n else {}
+            call = lambda space: P.spd_shared_attention(q[:rows], kc, vc, otab[:rows], i32([own] * rows), workspace=space, **kw)   # noqa: E731
+            assert torch.equal(call(ws), call(None))
