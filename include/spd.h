@@ -379,7 +379,8 @@ int spd_cache_append(const spd_append_args *args);
 /*
  * Attention for sequences that share prefixes.  n query rows of b sequences (rows q_start[s] .. q_start[s + 1] are
  * sequence s; q_start NULL: one row each, n = b) in g groups of neighbouring sequences (group_start[g + 1]; NULL: one group of
- * all).  Row i of sequence s, which has c rows, attends to all prefix_len[group] positions of its group's prefix and to
+ * all; a sequence in no group has no prefix).  Where q_start or group_start falls, no row sees anything and *status is SPD_ERANGE.
+ * Row i of sequence s, which has c rows, attends to all prefix_len[group] positions of its group's prefix and to
  * its own positions 0 .. own_len[s] - (c - 1 - i) - 1: the queries are the sequence's last c tokens, their keys already
  * in the cache.  out = sum(e^(scale q.k - m) v) / sum(e^(scale q.k - m)) over both; lse (may be NULL) [n][n_heads] float32 = log
  * of the sum of e^(scale q.k).  A row that sees nothing, or nothing but scores of minus infinity, gives zeros and

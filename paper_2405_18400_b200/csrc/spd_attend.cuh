@@ -63,7 +63,7 @@ struct Attend {
   float scale_log2;
   float *prefix_o, *own_o;      // parts: [part][rows][head_dim]
   float2 *prefix_ml, *own_ml;   // [part][rows]: maximum (in powers of two), sum
-  long long prefix_parts, own_parts;  // that the workspace holds: all of them, unless q_start or group_start is no partition
+  long long prefix_parts, own_parts;  // that the workspace holds: all of them, unless the arrays change under the kernel
   int blocks;                   // of the first launch
   int prefix_room, own_room;    // places of a table's row
   int many_parts;               // a row's prefix comes in six parts and more (1), in sixteen and more (2)
@@ -84,14 +84,15 @@ template <int MODE> constexpr int kPositions = kTf32<MODE> ? 8 : 16;
 // ---- work: how many steps and tiles a group's prefix and a sequence's own part are, and who does them.  Every warp works it out
 // for itself (32 segments at a time, no barrier); the host has made sure that all steps fit 31 bits.
 struct Cost {
-  int steps, tiles;
+  int steps, tiles;                // steps < 0: the segment ends before it begins
 };
 struct Totals {
   int steps, tiles;                // all of them
   int before, tiles_before;        // those of the segments in front of `mark`
+  bool falls;                      // the segments are no partition
 };
 
-// (Bounded, so that arrays that are no partition cannot lead outside the queries.)
+// (Bounded, so that no entry leads outside the queries; entries that do not fall are then a partition, whose steps the host has bounded.)
 __device__ __forceinline__ int within(int v, int most) { return v < 0 ? 0 : v < most ? v : most; }
 __device__ __forceinline__ int first_row(const Attend &p, int seq) { return p.a.q_start ? within(p.a.q_start[seq], p.a.n) : seq; }
 __device__ __forceinline__ int first_seq(const Attend &p, int g) { return p.a.group_start ? within(p.a.group_start[g], p.a.b) : g * p.a.b; }
@@ -101,8 +102,10 @@ __device__ __forceinline__ int own_length(const Attend &p, int s) { return withi
 
 template <int HEIGHT, int STEP>
 __device__ __forceinline__ Cost prefix_cost(const Attend &p, int g) {
+  const int first = first_seq(p, g), end = first_seq(p, g + 1);
+  if (end < first) return {-1, 0};
   const int steps = (int)(((unsigned)prefix_length(p, g) + STEP - 1) / STEP);
-  const int rows = (first_row(p, first_seq(p, g + 1)) - first_row(p, first_seq(p, g))) * p.ratio;
+  const int rows = (first_row(p, end) - first_row(p, first)) * p.ratio;
   const int tiles = steps ? tiles_of(rows, HEIGHT) * p.a.n_kv_heads : 0;
   return {tiles * steps, tiles};
 }
@@ -110,6 +113,7 @@ template <int STEP, int HEIGHT>
 __device__ __forceinline__ Cost own_cost(const Attend &p, int s) {
   const int steps = (int)(((unsigned)own_length(p, s) + STEP - 1) / STEP);
   const int rows = (first_row(p, s + 1) - first_row(p, s)) * p.ratio;
+  if (rows < 0) return {-1, 0};
   const int tiles = steps ? tiles_of(rows, HEIGHT) * p.a.n_kv_heads : 0;
   return {tiles * steps, tiles};
 }
@@ -117,19 +121,26 @@ __device__ __forceinline__ Cost own_cost(const Attend &p, int s) {
 template <typename F>
 __device__ __forceinline__ Totals sum_segments(int n, int mark, F cost) {
   const int lane = threadIdx.x & 31;
-  Totals t = {0, 0, 0, 0};
+  Totals t = {0, 0, 0, 0, false};
 #pragma unroll 1
   for (int base = 0; base < n; base += 32) {
     const int i = base + lane;
     const Cost c = i < n ? cost(i) : Cost{0, 0};
     t.steps += __reduce_add_sync(~0u, c.steps);
     t.tiles += __reduce_add_sync(~0u, c.tiles);
+    t.falls |= __any_sync(~0u, c.steps < 0);
     if (base < mark) {
       t.before += __reduce_add_sync(~0u, i < mark ? c.steps : 0);
       t.tiles_before += __reduce_add_sync(~0u, i < mark ? c.tiles : 0);
     }
   }
   return t;
+}
+// Nothing is attended to where q_start or group_start falls: the sums above say nothing then.
+__device__ __forceinline__ bool no_partition(Totals &pre, Totals &own) {
+  const bool falls = pre.falls || own.falls;
+  if (falls) pre.steps = own.steps = 0;
+  return falls;
 }
 
 // The segment that holds a step.
@@ -1118,12 +1129,13 @@ struct Attending {
     // the place of the next step to be looked up
     Place place = find_segment(a.b, at, cost);
     int token0 = 0, count = 0, len = 0, steps = 0, high = 0, tiles = 0;
+    int n = end - at;
+    int ahead = 0;               // steps looked up
     const auto enter = [&]() {   // the segment's numbers; empty ones are passed over
 #pragma unroll 1
       for (;;) {
-        if (place.segment >= a.b) {   // (only if the arrays change under the kernel: nothing to attend to)
-          token0 = count = len = 0, steps = high = 1, tiles = 0x7fffffff;
-          place.segment = a.b - 1;
+        if (place.segment >= a.b) {   // (only if the arrays change under the kernel: the run ends)
+          n = ahead, steps = high = 1;
           return;
         }
         token0 = first_row(p, place.segment);
@@ -1140,8 +1152,6 @@ struct Attending {
     };
     enter();
     int tile = (at - place.before) / steps, step = at - place.before - tile * steps, h = tile / high, row = tile - h * high;
-    const int n = end - at;
-    int ahead = 0;               // steps looked up
     int number = -1;
     const auto entry = [&]() {
       const int pos = step * kP + lane;
@@ -1236,8 +1246,8 @@ __global__ void __launch_bounds__(32 * NW, PER_SM) spd_attend_kernel(const __gri
   const spd_attention_args &a = p.a;
   const auto prefix = [&](int g) { return prefix_cost<kHeight, kStep>(p, g); };
   const auto own = [&](int s) { return own_cost<kPositions<MODE>, kRows<MODE>>(p, s); };
-  const Totals pre = sum_segments(a.g, 0, prefix);
-  const Totals mine = sum_segments(a.b, 0, own);
+  Totals pre = sum_segments(a.g, 0, prefix), mine = sum_segments(a.b, 0, own);
+  if (no_partition(pre, mine)) return;
   const Split split = split_blocks(gridDim.x, NW, p.weights, pre, mine);
   A w(p, smem_u32(dyn));
   if ((int)blockIdx.x < split.prefix_blocks) {
@@ -1300,8 +1310,9 @@ __global__ void __launch_bounds__(kJoinThreads) spd_attend_join_kernel(const __g
       const unsigned hit = __ballot_sync(~0u, g < a.g && a.group_start[g < a.g ? g : 0] <= seq && seq < a.group_start[g < a.g ? g + 1 : 0]);
       if (hit) group = base + __ffs(hit) - 1;
     }
-  const Totals pre = sum_segments(a.g, group, [&](int g) { return prefix_cost<HEIGHT, POS * NW>(p, g); });
-  const Totals own = sum_segments(a.b, seq, [&](int s) { return own_cost<POS, OWN>(p, s); });
+  Totals pre = sum_segments(a.g, group, [&](int g) { return prefix_cost<HEIGHT, POS * NW>(p, g); });
+  Totals own = sum_segments(a.b, seq, [&](int s) { return own_cost<POS, OWN>(p, s); });
+  const bool falls = no_partition(pre, own);
   const Split split = split_blocks(p.blocks, NW, p.weights, pre, own);
   const int h = p.by_ratio(head), hr = head - h * p.ratio;
   // pieces: prefix parts first .. first + np - 1 at row `prow`, own parts at `orow`
@@ -1335,7 +1346,7 @@ __global__ void __launch_bounds__(kJoinThreads) spd_attend_join_kernel(const __g
   }
   if (pfirst + np > p.prefix_parts) np = pfirst < p.prefix_parts ? (int)(p.prefix_parts - pfirst) : 0;
   if (ofirst + no > p.own_parts) no = ofirst < p.own_parts ? (int)(p.own_parts - ofirst) : 0;
-  if (a.status && lane == 0 && (seq < 0 || past_table(a.own_len[seq], p.own_room) || (group >= 0 && a.g > 0 && past_table(a.prefix_len[group], p.prefix_room))))
+  if (a.status && lane == 0 && (falls || seq < 0 || past_table(a.own_len[seq], p.own_room) || (group >= 0 && a.g > 0 && past_table(a.prefix_len[group], p.prefix_room))))
     *a.status = SPD_ERANGE;
   dep_wait();
   if (head >= a.n_heads) return;

@@ -101,3 +101,30 @@ def test_smaller_calls_in_a_larger_ones_workspace(x, kv, heads, kv_heads, dim):
             kw = dict(prefix_table=ptab[:n], prefix_len=i32([prefix] * n), prefix_page=10, group_start=i32([w * i for i in range(n + 1)])) if n else {}
             call = lambda space: P.spd_shared_attention(q[:rows], kc, vc, otab[:rows], i32([own] * rows), workspace=space, **kw)   # noqa: E731
             assert torch.equal(call(ws), call(None))
+
+
+# ---------------------------------------------------------------- attention: arrays that are no partition
+@pytest.mark.parametrize("x,kv", [(BF16, BF16), (F32, BF16), (F32, F32)])
+def test_where_rows_or_groups_fall_nothing_is_seen(x, kv):
+    g = gen(11)
+    h, d, slots, b = 4, 64, 300, 5
+    kc, vc, q = normal(g, slots, h, d).to(kv), normal(g, slots, h, d).to(kv), normal(g, 9, h, d).to(x)
+    ptab = torch.randint(0, slots, (2, 70), generator=g, device=DEV).to(torch.int32)
+    otab = torch.randint(0, slots, (b, 20), generator=g, device=DEV).to(torch.int32)
+    good = ([0, 2, 4, 4, 6, 9], [0, 2, 5])
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def call(rows, groups):
+        status.zero_()
+        return P.spd_shared_attention(q, kc, vc, otab, i32([20] * b), prefix_table=ptab, prefix_len=i32([70, 33]), group_start=i32(groups), q_start=i32(rows),
+                                      return_lse=True, status=status)
+    want = call(*good)
+    assert int(status) == 0
+    for rows, groups in (([5, 6, 0, 3, 6, 9], good[1]), ([1, 2, 0, 9, 9, 9], good[1]), ([0, 9, 0, 9, 0, 9], good[1]), ([0, 2, 4, 4, 9, 7], good[1]),
+                         (good[0], [2, 0, 5]), (good[0], [0, 5, 1]), ([9, 7, 5, 3, 1, 0], [5, 3, 0])):
+        out, lse = call(rows, groups)
+        assert int(status) == -3 and not out.any() and (lse == -math.inf).all()
+    out, lse = call([-4, 2, 4, 4, 6, 1000], [-1, 2, 70])       # entries outside the rows and sequences, in order: as far as they lie inside
+    assert torch.equal(out[4:6], want[0][4:6]) and int(status) == 0
+    again = call(*good)
+    assert int(status) == 0 and all(torch.equal(a, b) for a, b in zip(want, again))
