@@ -104,6 +104,11 @@ void rows_of(const at::Tensor &t, int device, const char *what, int64_t *row, in
   on(device, t);
   *row = t.stride(0), *head = t.stride(1);
 }
+// A workspace: what the call may write is its bytes, which have to be there (a view that repeats elements counts more).
+void room(const at::Tensor &t, int device) {
+  if (!t.is_contiguous()) refuse("workspace: a contiguous tensor expected");
+  on(device, t);
+}
 void *data(const at::Tensor &t) { return const_cast<void *>(t.const_data_ptr()); }
 
 void check(int rc, const char *name) {
@@ -288,7 +293,7 @@ PyObject *shared_attention(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     const c10::cuda::CUDAGuard guard(device);
     if (given(a[14])) {
       space = tensor(a[14], "workspace: a tensor expected");
-      on(device, space);
+      room(space, device);
     } else {
       size_t bytes = 0;
       check(g_attention_bytes(&p, &bytes), "spd_shared_attention_bytes");
@@ -348,7 +353,7 @@ PyObject *beam_select(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     if (given(a[3])) p.ended = static_cast<const uint8_t *>(data(per_beam(a[3], z, device, at::kBool, "finished: contiguous bool [requests, beams] on the logits' device expected")));
     p.eos_id = int32(a[4]), p.tau = real(a[5]), p.alpha = real(a[6]);
     const at::Tensor &space = tensor(a[7], "workspace: a tensor expected");
-    on(device, space);
+    room(space, device);
     const int64_t shape[2] = {z.size(0), z.size(1)};
     at::Tensor out[5] = {empty(shape, at::kInt, z), empty(shape, at::kInt, z), empty(shape, at::kFloat, z), empty(shape, at::kInt, z), empty(shape, at::kBool, z)};
     p.logits = data(z), p.score = static_cast<const float *>(data(score));

@@ -128,3 +128,17 @@ def test_where_rows_or_groups_fall_nothing_is_seen(x, kv):
     assert torch.equal(out[4:6], want[0][4:6]) and int(status) == 0
     again = call(*good)
     assert int(status) == 0 and all(torch.equal(a, b) for a, b in zip(want, again))
+
+
+# ---------------------------------------------------------------- refusals
+def test_workspaces_that_repeat_their_elements_are_refused():
+    """A view of a few bytes may count as many: only those that are there may be written."""
+    q, kc, table = torch.zeros(3, 2, 64, device=DEV), torch.zeros(8, 2, 64, device=DEV), i32([[0], [1], [2]])
+    z, score = torch.zeros(2, 3, 10, device=DEV), torch.zeros(2, 3, device=DEV)
+    few = torch.zeros(64, dtype=torch.uint8, device=DEV)
+    for space in (few[:1].expand(1 << 26), few[:1, None].expand(1, 1 << 26), few.view(2, 32).t()):
+        with pytest.raises(ValueError):
+            P.spd_shared_attention(q, kc, kc.clone(), table, i32([1, 1, 1]), workspace=space)
+        with pytest.raises(ValueError):
+            P.spd_beam_select(z, score, workspace=space)
+    assert not few.any()
