@@ -213,6 +213,7 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     p.index = ints(a[8], p.n, device, "index: contiguous int32, one per token, expected");
     p.seq = ints(a[9], p.n, device, "seq: contiguous int32, one per token, expected");
     const Table t = table(a[10], device, "table: int32 [sequences, pages] with contiguous rows expected");
+    if (given(a[10]) && p.n && (!t.rows || !t.cols)) refuse("table: at least one page expected");   // (a null table would make places slots)
     p.table = t.at, p.table_row = t.row, p.table_rows = t.rows, p.table_cols = t.cols;
     p.page = int32(a[11]), p.pairs = int32(a[12]);
     if (given(a[5])) {

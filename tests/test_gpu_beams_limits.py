@@ -142,3 +142,14 @@ def test_workspaces_that_repeat_their_elements_are_refused():
         with pytest.raises(ValueError):
             P.spd_beam_select(z, score, workspace=space)
     assert not few.any()
+
+
+def test_an_append_to_a_table_without_pages_is_refused():
+    """An empty tensor has no address, and no table means that places are slots: nothing may go there."""
+    x, pos = torch.ones(2, 1, 8, device=DEV), i32([0, 1])
+    for shape in ((0, 4), (2, 0), (0, 0)):
+        kc, vc = torch.zeros(6, 1, 8, device=DEV), torch.zeros(6, 1, 8, device=DEV)
+        with pytest.raises(ValueError):
+            P.spd_cache_append(x, x, kc, vc, pos, None, table=torch.empty(shape, dtype=torch.int32, device=DEV))
+        assert not kc.any() and not vc.any()
+    P.spd_cache_append(x[:0], x[:0], kc, vc, pos[:0], None, table=torch.empty(0, 0, dtype=torch.int32, device=DEV))   # no tokens: no pages needed
