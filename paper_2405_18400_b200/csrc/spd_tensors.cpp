@@ -45,6 +45,11 @@ long integer(PyObject *o) {
   if (v == -1 && PyErr_Occurred()) throw Raised();
   return v;
 }
+bool truth(PyObject *o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Raised();
+  return v != 0;
+}
 int32_t int32(PyObject *o) {
   const long v = integer(o);
   if (v < INT32_MIN || v > INT32_MAX) refuse("an argument does not fit 32 bits");
@@ -283,7 +288,7 @@ PyObject *shared_attention(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     at::Tensor out = given(a[12]) ? tensor(a[12], "out: a tensor expected") : empty(q.sizes(), q.scalar_type(), q), lse, space;
     rows_of(out, device, "out: [rows, heads, dim] with a contiguous last dimension expected", &p.o_row, &p.o_head);
     if (out.sizes() != q.sizes() || out.scalar_type() != q.scalar_type()) refuse("out and q disagree in shape or type");
-    const bool with_lse = a[13] == Py_True;
+    const bool with_lse = truth(a[13]);
     if (with_lse) {
       lse = empty({q.size(0), q.size(1)}, at::kFloat, q);
       p.lse = static_cast<float *>(data(lse));

@@ -153,3 +153,13 @@ def test_an_append_to_a_table_without_pages_is_refused():
             P.spd_cache_append(x, x, kc, vc, pos, None, table=torch.empty(shape, dtype=torch.int32, device=DEV))
         assert not kc.any() and not vc.any()
     P.spd_cache_append(x[:0], x[:0], kc, vc, pos[:0], None, table=torch.empty(0, 0, dtype=torch.int32, device=DEV))   # no tokens: no pages needed
+
+
+def test_return_lse_is_any_truth_value():
+    q, kc, table = torch.ones(3, 2, 64, device=DEV), torch.ones(8, 2, 64, device=DEV), i32([[0], [1], [2]])
+    call = lambda lse: P.spd_shared_attention(q, kc, kc.clone(), table, i32([1, 1, 1]), return_lse=lse)   # noqa: E731
+    for yes in (True, 1, "yes", [0], torch.ones(1)):
+        out, lse = call(yes)
+        assert out.shape == q.shape and lse.shape == (3, 2)
+    for no in (False, 0, None, ""):
+        assert torch.equal(call(no), out)
