@@ -448,8 +448,9 @@ int spd_beam_select_bytes(const spd_select_args *args, size_t *bytes);
 /*
  * The beams' states follow their parents, in place: row (o, r, j) becomes what row (o, r, parent[r][j]) was before the
  * call, for every o < outer, request r and beam j.  Up to SPD_MAX_STATES arrays in one launch, each with rows of row_bytes contiguous bytes
- * at state + o * outer_stride + r * request_stride + j * beam_stride (bytes; rows must not overlap).  parent [requests][beams]
- * contiguous.  1 <= beams <= 32.  A row that keeps its beam is neither read for itself nor written.
+ * at state + o * outer_stride + r * request_stride + j * beam_stride (bytes).  No two rows of a call may overlap: a stride shorter than
+ * a row and a state given twice are SPD_EINVAL.  parent [requests][beams] contiguous.  1 <= beams <= 32.  A row that keeps its beam is neither
+ * read for itself nor written.
  */
 #define SPD_MAX_STATES 8
 typedef struct {

@@ -100,6 +100,7 @@ def spd_beam_select(logits: torch.Tensor, score: torch.Tensor, length: Optional[
 def spd_beam_reorder(states: Union[torch.Tensor, Sequence[torch.Tensor]], parent: torch.Tensor, *, dim: int = 0,
                      status: Optional[torch.Tensor] = None) -> None:
     """In place: beam j of request r becomes what beam parent[r, j] was, in every state.  A state has requests and beams as its
-    dimensions `dim` and `dim` + 1; those behind are contiguous (a view of the first steps will do), those in front have one stride."""
+    dimensions `dim` and `dim` + 1; those behind are contiguous (a view of the first steps will do), those in front have one stride.  No element may
+    be there twice, in a state or in two of them."""
     states = (states,) if isinstance(states, torch.Tensor) else tuple(states)
     (_tensors or load_tensors()).beam_reorder(states, parent, dim, status)

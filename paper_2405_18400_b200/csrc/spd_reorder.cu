@@ -89,8 +89,8 @@ extern "C" int spd_beam_reorder(const spd_reorder_args *args) {
   for (int i = 0; i < a.n_states; ++i) {
     if (a.outer[i] == 0 || a.row_bytes[i] == 0) continue;
     if (!a.state[i] || a.outer[i] < 0 || a.row_bytes[i] < 0) return SPD_EINVAL;
-    const int64_t span = a.beam_stride[i] < 0 ? -a.beam_stride[i] : a.beam_stride[i];
-    if (a.beams > 1 && span < a.row_bytes[i]) return SPD_EINVAL;  // beams that overlap
+    const auto apart = [&](int64_t stride) { return (stride < 0 ? -stride : stride) >= a.row_bytes[i]; };
+    if (a.beams > 1 && !apart(a.beam_stride[i])) return SPD_EINVAL;
     ReorderState &s = p.st[p.n_states++];
     s.base = static_cast<char *>(a.state[i]);
     s.outer_stride = a.outer_stride[i];
@@ -103,6 +103,10 @@ extern "C" int spd_beam_reorder(const spd_reorder_args *args) {
     s.first_block = blocks;
     const __int128 more = (__int128)s.col_blocks * a.outer[i] * a.requests;
     if (more + blocks > 0x7fffffff) return SPD_ERANGE;
+    // Blocks that write the same rows would read what one another wrote.
+    if (a.beams > 1 && ((a.requests > 1 && !apart(a.request_stride[i])) || (a.outer[i] > 1 && !apart(a.outer_stride[i])))) return SPD_EINVAL;
+    for (int j = 0; a.beams > 1 && j + 1 < p.n_states; ++j)
+      if (p.st[j].base == s.base) return SPD_EINVAL;
     blocks += (int64_t)more;
   }
   if (blocks == 0 || a.beams == 1) return SPD_OK;

@@ -10,9 +10,11 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <stdexcept>
+#include <vector>
 
 #include "spd.h"
 
@@ -401,7 +403,13 @@ PyObject *beam_reorder(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     const c10::cuda::CUDAGuard guard(device);
     const Py_ssize_t n = PySequence_Fast_GET_SIZE(a[0]);
     PyObject **items = PySequence_Fast_ITEMS(a[0]);
-    for (int launch = 0; launch < 2; ++launch)  // all states are looked over before the first is touched
+    std::vector<const void *> starts;   // of the states that have rows to move
+    const auto apart = [](int64_t stride, int64_t row) { return (stride < 0 ? -stride : stride) >= row; };
+    for (int launch = 0; launch < 2; ++launch) {  // all states are looked over before the first is touched
+      if (launch) {
+        std::sort(starts.begin(), starts.end());
+        if (std::adjacent_find(starts.begin(), starts.end()) != starts.end()) refuse("a state given twice");
+      }
       for (Py_ssize_t first = 0; first < n; first += SPD_MAX_STATES) {
         p.n_states = (int32_t)(n - first < SPD_MAX_STATES ? n - first : SPD_MAX_STATES);
         for (int i = 0; i < p.n_states; ++i) {
@@ -420,12 +428,17 @@ PyObject *beam_reorder(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
             else if (t.stride(k) != outer * step) refuse("a state's dimensions in front of the requests need one stride");
             outer *= t.size(k);
           }
+          if (!launch && w > 1 && t.numel()) {
+            if (!apart(t.stride(dim + 1), row) || (r > 1 && !apart(t.stride(dim), row)) || (outer > 1 && !apart(step, row))) refuse("a state's rows lie on one another");
+            starts.push_back(t.const_data_ptr());
+          }
           p.state[i] = data(t);
           p.outer[i] = outer, p.outer_stride[i] = step * size, p.request_stride[i] = t.stride(dim) * size, p.beam_stride[i] = t.stride(dim + 1) * size;
           p.row_bytes[i] = row * size;
         }
         if (launch) check(g_reorder(&p), "spd_beam_reorder");
       }
+    }
     Py_RETURN_NONE;
   });
 }

@@ -1,0 +1,15 @@
+"""More of what the beams' operators refuse, without a GPU: the library's argument checks come before any CUDA call."""
+import ctypes as C
+
+from tests.test_beams_host import A8, A8L, AT, EINVAL, Reorder, lib, refused   # noqa: F401
+
+
+def test_states_that_lie_on_one_another_are_refused(lib):   # noqa: F811
+    """Rows that two blocks write while a third reads them: a request or outer stride shorter than a row, a state given twice."""
+    base = dict(state=A8(*[AT + 4096 * i for i in range(8)]), outer=A8L(*[2] * 8), outer_stride=A8L(*[256] * 8), request_stride=A8L(*[64] * 8),
+                beam_stride=A8L(*[16] * 8), row_bytes=A8L(*[16] * 8), parent=AT, n_states=1, requests=2, beams=4)
+    twice = A8(*[AT + 4096 * min(i, 1) for i in range(8)])
+    refused(lib, "spd_beam_reorder", Reorder, base, [
+        (EINVAL, dict(request_stride=A8L(*[0] * 8))), (EINVAL, dict(outer_stride=A8L(*[0] * 8))), (EINVAL, dict(request_stride=A8L(*[-15] * 8))),
+        (EINVAL, dict(outer_stride=A8L(*[8] * 8))), (EINVAL, dict(n_states=2, state=A8(*[AT] * 8))), (EINVAL, dict(n_states=3, state=twice)),
+        (0, dict(beams=1, request_stride=A8L(*[0] * 8)))])

@@ -163,3 +163,21 @@ def test_return_lse_is_any_truth_value():
         assert out.shape == q.shape and lse.shape == (3, 2)
     for no in (False, 0, None, ""):
         assert torch.equal(call(no), out)
+
+
+def test_states_that_lie_on_one_another_are_refused():
+    parent = i32([[1, 0], [1, 1]])
+    one, other = torch.arange(8.0, device=DEV).view(2, 2, 2), torch.arange(8.0, device=DEV).view(2, 2, 2)
+    row = torch.arange(2.0, device=DEV)
+    wide = torch.arange(12.0, device=DEV)
+    layers = one.expand(3, 2, 2, 2)
+    many = [torch.arange(8.0, device=DEV).view(2, 2, 2) for _ in range(10)]
+    for states, dim in (([one, one], 0), ([one, other, one], 0), (row.expand(2, 2, 2), 0), (one[:1].expand(2, 2, 2), 0), (layers, 1),
+                        (wide.as_strided((2, 2, 2), (4, 1, 1)), 0), (many + [many[0]], 0)):
+        with pytest.raises(ValueError):
+            P.spd_beam_reorder(states, parent, dim=dim)
+    assert all(t.flatten().tolist() == list(range(8)) for t in [one, other] + many)
+    pair = torch.arange(16.0, device=DEV).view(2, 2, 2, 2)                    # two states side by side in one buffer lie apart
+    P.spd_beam_reorder([pair[:, :, 0], pair[:, :, 1]], parent)
+    assert pair.flatten().tolist() == [4, 5, 6, 7, 0, 1, 2, 3, 12, 13, 14, 15, 12, 13, 14, 15]
+    P.spd_beam_reorder([row.view(1, 1, 2).expand(2, 1, 2)], i32([[0], [0]]))   # one beam: nothing moves
