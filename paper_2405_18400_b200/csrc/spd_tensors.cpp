@@ -111,6 +111,11 @@ void rows_of(const at::Tensor &t, int device, const char *what, int64_t *row, in
   on(device, t);
   *row = t.stride(0), *head = t.stride(1);
 }
+// The same of a tensor that is written: no element may be there twice.
+void written(const at::Tensor &t, int device, const char *what, int64_t *row, int64_t *head) {
+  rows_of(t, device, what, row, head);
+  if ((*row == 0 && t.size(0) > 1) || (*head == 0 && t.size(1) > 1)) refuse("a tensor that is written repeats its elements");
+}
 // A workspace: what the call may write is its bytes, which have to be there (a view that repeats elements counts more).
 void room(const at::Tensor &t, int device) {
   if (!t.is_contiguous()) refuse("workspace: a contiguous tensor expected");
@@ -195,7 +200,7 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
       const at::Tensor &q = tensor(a[6], "q: a tensor expected");
       rows_of(q, device, "q: [tokens, heads, dim] with a contiguous last dimension expected", &p.q_row, &p.q_head);
       out = given(a[7]) ? tensor(a[7], "q_out: a tensor expected") : empty(q.sizes(), q.scalar_type(), q);
-      rows_of(out, device, "q_out: [tokens, heads, dim] with a contiguous last dimension expected", &p.qo_row, &p.qo_head);
+      written(out, device, "q_out: [tokens, heads, dim] with a contiguous last dimension expected", &p.qo_row, &p.qo_head);
       if (q.size(0) != p.n || q.size(2) != p.head_dim || out.sizes() != q.sizes() || q.scalar_type() != lead.scalar_type() || out.scalar_type() != lead.scalar_type())
         refuse("q, q_out and k disagree in shape or type");
       p.n_heads = size32(q.size(1));
@@ -205,8 +210,8 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
       const at::Tensor &v = tensor(a[1], "v: a tensor expected"), &kc = tensor(a[2], "k_cache: a tensor expected"), &vc = tensor(a[3], "v_cache: a tensor expected");
       rows_of(lead, device, "k: [tokens, heads, dim] with a contiguous last dimension expected", &p.k_row, &p.k_head);
       rows_of(v, device, "v: [tokens, heads, dim] with a contiguous last dimension expected", &p.v_row, &p.v_head);
-      rows_of(kc, device, "k_cache: [slots, heads, dim] with a contiguous last dimension expected", &p.kc_slot, &p.kc_head);
-      rows_of(vc, device, "v_cache: [slots, heads, dim] with a contiguous last dimension expected", &p.vc_slot, &p.vc_head);
+      written(kc, device, "k_cache: [slots, heads, dim] with a contiguous last dimension expected", &p.kc_slot, &p.kc_head);
+      written(vc, device, "v_cache: [slots, heads, dim] with a contiguous last dimension expected", &p.vc_slot, &p.vc_head);
       p.kv_dtype = type_of(kc, "caches: float32 or bfloat16 expected");
       if (v.sizes() != lead.sizes() || v.scalar_type() != lead.scalar_type() || vc.sizes() != kc.sizes() || vc.scalar_type() != kc.scalar_type() ||
           kc.size(1) != lead.size(1) || kc.size(2) != lead.size(2))
@@ -288,7 +293,7 @@ PyObject *shared_attention(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     p.q_start = ints(a[10], (int64_t)p.b + 1, device, "q_start: contiguous int32, one per sequence and one more, expected");
     p.scale = given(a[11]) ? real(a[11]) : 1.f / std::sqrt((float)p.head_dim);
     at::Tensor out = given(a[12]) ? tensor(a[12], "out: a tensor expected") : empty(q.sizes(), q.scalar_type(), q), lse, space;
-    rows_of(out, device, "out: [rows, heads, dim] with a contiguous last dimension expected", &p.o_row, &p.o_head);
+    written(out, device, "out: [rows, heads, dim] with a contiguous last dimension expected", &p.o_row, &p.o_head);
     if (out.sizes() != q.sizes() || out.scalar_type() != q.scalar_type()) refuse("out and q disagree in shape or type");
     const bool with_lse = truth(a[13]);
     if (with_lse) {

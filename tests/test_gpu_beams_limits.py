@@ -181,3 +181,18 @@ def test_states_that_lie_on_one_another_are_refused():
     P.spd_beam_reorder([pair[:, :, 0], pair[:, :, 1]], parent)
     assert pair.flatten().tolist() == [4, 5, 6, 7, 0, 1, 2, 3, 12, 13, 14, 15, 12, 13, 14, 15]
     P.spd_beam_reorder([row.view(1, 1, 2).expand(2, 1, 2)], i32([[0], [0]]))   # one beam: nothing moves
+
+
+def test_outputs_that_repeat_their_elements_are_refused():
+    x, pos, table = torch.zeros(3, 2, 64, device=DEV), i32([0, 1, 2]), i32([[0], [1], [2]])
+    cache = torch.zeros(8, 2, 64, device=DEV)
+    for twice in (cache[:1].expand(8, 2, 64), cache[:, :1].expand(8, 2, 64)):
+        for caches in ((twice, cache), (cache, twice)):
+            with pytest.raises(ValueError):
+                P.spd_cache_append(x, x, *caches, pos, None, index=pos)
+        with pytest.raises(ValueError):
+            P.spd_cache_append(None, None, None, None, pos, None, q=x, q_out=twice[:3])
+        with pytest.raises(ValueError):
+            P.spd_shared_attention(x, cache, cache, table, i32([1, 1, 1]), out=twice[:3])
+        P.spd_shared_attention(twice[:3], twice, twice, table, i32([1, 1, 1]))     # what is read may be
+        P.spd_cache_append(twice[:3], twice[:3], cache, cache.clone(), pos, None, q=twice[:3], index=pos)
