@@ -421,7 +421,7 @@ int spd_shared_attention_bytes(const spd_attention_args *args, size_t *bytes);
  * then the lower token's; new_parent says which beam each extends.  A new beam has ended when its parent had or its token is eos_id (-1: none).  Logits of minus infinity
  * and NaN are no options and have no weight; a row whose largest is not finite has none, nor does a beam whose score is NaN.
  * Where fewer options than beams exist, the rest gets token -1, parent = its own number, score minus infinity, length 0, not ended.
- * The rank is decided in 64 bits.  1 <= beams <= 32, vocab <= 262144.  length and ended may be NULL (zeros), new_length and
+ * The rank is decided in 64 bits.  tau > 0 (infinite: all tokens alike), alpha >= 0 and finite.  1 <= beams <= 32, vocab <= 262144.  length and ended may be NULL (zeros), new_length and
  * new_ended too; they are [requests][beams] and contiguous, as score and new_*, which must not overlap what is read.  workspace: spd_beam_select_bytes of DEVICE
  * memory, 256-byte aligned, zeroed once before its first use (calls leave its counters at zero, and no call's data lies where
  * another's counters do) and not shared by calls that overlap.  It serves calls of as many requests or fewer, and whatever else needs no more bytes.

@@ -10,6 +10,9 @@
 // these w lists can be among the w best of all.  So with four lanes' logits as a list, the w-th best head is a threshold, and
 // what passes it (a few more than w on random rows) is ranked by counting the greater ones.  Sorted lists are then merged, by counting too where
 // they are few, else by taking the best head w times.  A key holds value and index, so that no two are equal and ties fall to the lower index.
+#include <cfloat>
+#include <cmath>
+
 #include <math_constants.h>
 
 #include "spd_ops.h"
@@ -112,7 +115,8 @@ struct Shared {
   unsigned long long threshold;
   float limit_value, wsum[kSelWarps];
   int count, last;
-  double at[kSelMaxBeams];                                 // of a beam: score - largest logit / tau - log sum
+  double at[kSelMaxBeams];                                 // of a beam: score - log sum, the value of its largest logit
+  float most[kSelMaxBeams];                                // that logit
   double per[kSelMaxBeams], inv_per[kSelMaxBeams];         // length^alpha and its inverse
   float score[kSelMaxBeams];
   int length[kSelMaxBeams];
@@ -323,7 +327,8 @@ __device__ __forceinline__ void select_join(const Select &p, Shared &sh, Option 
     for (int j = lanes >> 1; j > 0; j >>= 1) s += __shfl_xor_sync(~0u, s, j);
     if (here && list == 0) {
       // A row whose largest logit is not finite, or a sum that is not, gives no number here and has no options.
-      sh.at[i] = ended ? (double)score : (double)score - (double)m * p.inv_tau - log_of_sum(s);
+      sh.at[i] = ended ? (double)score : (double)score - log_of_sum(s);
+      sh.most[i] = m;
       sh.per[i] = per.x, sh.inv_per[i] = per.y;
       sh.score[i] = score, sh.length[i] = length, sh.ended[i] = ended, sh.in_use[i] = score > -CUDART_INF_F;
     }
@@ -369,7 +374,8 @@ __device__ __forceinline__ void select_join(const Select &p, Shared &sh, Option 
       const bool ended = sh.ended[i];
       const unsigned long long key = best[i * W + lane];
       if (ended ? lane == 0 : key != 0) {
-        const double z = ended ? 0.0 : (double)unordered((uint32_t)(key >> 32)) * p.inv_tau, rank = (sh.at[i] + z) * sh.inv_per[i];
+        // (the difference is exact: a score does not vanish beside logits of any size over any tau)
+        const double z = ended ? 0.0 : ((double)unordered((uint32_t)(key >> 32)) - (double)sh.most[i]) * p.inv_tau, rank = (sh.at[i] + z) * sh.inv_per[i];
         if (rank > -CUDART_INF) o.rank = ordered(rank), o.flat = (uint32_t)i * a.vocab + (ended ? max(a.eos_id, 0) : ~(uint32_t)key);
       }
     }
@@ -532,7 +538,7 @@ extern "C" int spd_beam_select(const spd_select_args *args) {
   const spd_select_args &a = *args;
   if (a.requests == 0) return SPD_OK;
   if (!a.logits || !a.score || !a.new_token || !a.new_parent || !a.new_score || !a.workspace || !aligned(a.workspace, 256)) return SPD_EINVAL;
-  if (!(a.tau > 0.f) || !(a.alpha >= 0.f) || a.eos_id < -1 || a.eos_id >= a.vocab || !aligned(a.logits, type_bytes(a.x_dtype))) return SPD_EINVAL;
+  if (!(a.tau > 0.f) || !(a.alpha >= 0.f) || std::isinf(a.alpha) || a.eos_id < -1 || a.eos_id >= a.vocab || !aligned(a.logits, type_bytes(a.x_dtype))) return SPD_EINVAL;
   const SelectPlan l = select_plan(a, aligned(a.logits, 16) && (a.request_stride | a.beam_stride) % (16 / (int64_t)type_bytes(a.x_dtype)) == 0);
   if (a.workspace_bytes < (int64_t)l.bytes) return SPD_ENOMEM;
   Select p;
@@ -540,7 +546,9 @@ extern "C" int spd_beam_select(const spd_select_args *args) {
   p.slices = l.slices;
   p.keys_fit = l.keys_fit;
   p.inv_tau = 1.0 / (double)a.tau;
-  p.scale = (float)(1.4426950408889634 / (double)a.tau);
+  // (kept finite and off zero: what is largest has weight 1 whatever tau is, what is masked none)
+  const double scale = 1.4426950408889634 / (double)a.tau;
+  p.scale = scale > (double)FLT_MAX ? FLT_MAX : scale < (double)FLT_TRUE_MIN ? FLT_TRUE_MIN : (float)scale;
   char *ws = static_cast<char *>(a.workspace);
   p.arrived = reinterpret_cast<unsigned *>(ws);
   p.stats = reinterpret_cast<float2 *>(ws + l.stats);

@@ -1,7 +1,7 @@
 """More of what the beams' operators refuse, without a GPU: the library's argument checks come before any CUDA call."""
-import ctypes as C
+import math
 
-from tests.test_beams_host import A8, A8L, AT, EINVAL, Reorder, lib, refused   # noqa: F401
+from tests.test_beams_host import A8, A8L, AT, EINVAL, Reorder, Select, lib, refused   # noqa: F401
 
 
 def test_states_that_lie_on_one_another_are_refused(lib):   # noqa: F811
@@ -13,3 +13,9 @@ def test_states_that_lie_on_one_another_are_refused(lib):   # noqa: F811
         (EINVAL, dict(request_stride=A8L(*[0] * 8))), (EINVAL, dict(outer_stride=A8L(*[0] * 8))), (EINVAL, dict(request_stride=A8L(*[-15] * 8))),
         (EINVAL, dict(outer_stride=A8L(*[8] * 8))), (EINVAL, dict(n_states=2, state=A8(*[AT] * 8))), (EINVAL, dict(n_states=3, state=twice)),
         (0, dict(beams=1, request_stride=A8L(*[0] * 8)))])
+
+
+def test_an_infinite_power_of_the_length_is_refused(lib):   # noqa: F811
+    base = dict(logits=AT, score=AT, new_token=AT, new_parent=AT, new_score=AT, workspace=AT, workspace_bytes=1 << 40, requests=2, beams=4, vocab=100,
+                x_dtype=0, eos_id=-1, tau=1.0, request_stride=400, beam_stride=100)
+    refused(lib, "spd_beam_select", Select, base, [(EINVAL, dict(alpha=math.inf)), (EINVAL, dict(tau=-math.inf)), (0, dict(requests=0))])

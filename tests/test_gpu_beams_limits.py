@@ -196,3 +196,32 @@ def test_outputs_that_repeat_their_elements_are_refused():
             P.spd_shared_attention(x, cache, cache, table, i32([1, 1, 1]), out=twice[:3])
         P.spd_shared_attention(twice[:3], twice, twice, table, i32([1, 1, 1]))     # what is read may be
         P.spd_cache_append(twice[:3], twice[:3], cache, cache.clone(), pos, None, q=twice[:3], index=pos)
+
+
+# ---------------------------------------------------------------- selection: temperatures of any size
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_select_at_an_infinite_temperature(dtype):
+    """All tokens that are options are alike; in a beam the larger logit stands first all the same."""
+    g = gen(21)
+    w, v = 3, 5000
+    z = normal(g, 1, w, v).to(dtype)
+    z[0, :, 100:4900] = -math.inf
+    score = torch.tensor([[-0.25, -1.0, -0.5]], device=DEV)
+    token, parent, new, _, _ = P.spd_beam_select(z, score, tau=math.inf)
+    order = torch.sort(z[0, 0].float(), descending=True, stable=True).indices[:w]
+    assert token[0].tolist() == order.tolist() and parent[0].tolist() == [0, 0, 0]
+    assert (new[0].double() + 0.25 + math.log(200)).abs().max() <= 2.0 ** -23 * 16
+
+
+def test_select_at_a_temperature_near_zero():
+    """1 / tau is past float32: the largest logit has all the weight, shared by those that equal it."""
+    w, v = 3, 5000
+    z = torch.zeros(1, w, v, device=DEV)
+    z[0, 0, [7, 4000]] = 0.01
+    z[0, 1, 55] = 0.01
+    z[0, 2] = -math.inf
+    z[0, 2, 9] = -5.0
+    score = torch.tensor([[-1.0, -2.0, -3.0]], device=DEV)
+    token, parent, new, _, _ = P.spd_beam_select(z, score, tau=1e-39)
+    assert list(zip(parent[0].tolist(), token[0].tolist())) == [(0, 7), (0, 4000), (1, 55)]
+    assert (new[0].double() - torch.tensor([-1 - math.log(2), -1 - math.log(2), -2.0], device=DEV)).abs().max() <= 2.0 ** -23 * 18
