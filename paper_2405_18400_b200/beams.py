@@ -9,6 +9,8 @@ their last dimension is contiguous.  Tensors that do not fit one another raise V
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
+import os
 from typing import Optional, Sequence, Union
 
 import torch
@@ -21,20 +23,23 @@ _tensors = None
 
 
 def load_tensors():
-    """The module that takes tensors to the operators, built first when its source is newer, tied to the loaded library."""
+    """The module that takes tensors to the operators, built first when its source is newer or none is there for this Python and torch, tied
+    to the loaded library."""
     global _tensors
     if _tensors is None:
-        library = load_library()
+        library, path = load_library(), _build.tensors_path()
         try:
             _build.build_tensors()
         except Exception as exc:  # no compiler on this machine: the prebuilt module must be there
-            if not _build.os.path.exists(_build.TENSORS):
-                raise RuntimeError("_spd_tensors.so is missing and could not be built: %s" % exc) from exc
-        from . import _spd_tensors
-        _spd_tensors.bind(*[C.cast(getattr(library, name), C.c_void_p).value for name in (
+            if not os.path.exists(path):
+                raise RuntimeError("%s is missing and could not be built: %s" % (os.path.basename(path), exc)) from exc
+        spec = importlib.util.spec_from_file_location(__package__ + "._spd_tensors", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(*[C.cast(getattr(library, name), C.c_void_p).value for name in (
             "spd_cache_append", "spd_shared_attention", "spd_shared_attention_bytes", "spd_beam_select", "spd_beam_select_bytes", "spd_beam_reorder")],
-                          _check, torch.OutOfMemoryError)
-        _tensors = _spd_tensors
+                    _check, torch.OutOfMemoryError)
+        _tensors = module
     return _tensors
 
 

@@ -12,7 +12,6 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libspd.so")
-TENSORS = os.path.join(HERE, "_spd_tensors.so")      # torch tensors in and out of the beams' operators
 SOURCES = ["spd_kernel.cu", "spd_prefill.cu", "spd_prefill_tc.cu", "spd_batch.cu", "spd_api.cu", "spd_ngram.cu",
            "spd_append.cu", "spd_attend.cu", "spd_attend_bf16.cu", "spd_attend_terms.cu", "spd_attend_few.cu", "spd_attend_few_float.cu", "spd_attend_eight.cu", "spd_attend_float.cu", "spd_select.cu",
            "spd_reorder.cu"]
@@ -25,23 +24,31 @@ def _nvcc() -> str:
     return exe
 
 
+def tensors_path() -> str:
+    """The module that takes torch tensors to the beams' operators: a file of its own for each Python and torch, whose layouts are compiled into it."""
+    import torch
+
+    return os.path.join(HERE, "_spd_tensors-%s-torch%s.so" % (sysconfig.get_config_var("SOABI"), torch.__version__))
+
+
 def _stale(target: str = LIB) -> bool:
     if not os.path.exists(target):
         return True
     t = os.path.getmtime(target)
     own = "spd_tensors.cpp"
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if (f == own) == (target == TENSORS)] + [os.path.join(INCLUDE, "spd.h")]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if (f == own) == (target != LIB)] + [os.path.join(INCLUDE, "spd.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
 def build_tensors(force: bool = False) -> str:
     """Builds the module that takes torch tensors to the operators (a C++ compiler and torch's headers, no GPU code)."""
-    if not force and not _stale(TENSORS):
-        return TENSORS
+    target = tensors_path()
+    if not force and not _stale(target):
+        return target
     import torch
     from torch.utils.cpp_extension import include_paths, library_paths
 
-    tmp = TENSORS + ".tmp%d" % os.getpid()
+    tmp = target + ".tmp%d" % os.getpid()
     cuda = os.path.dirname(os.path.dirname(_nvcc()))
     cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-I", INCLUDE]
     for path in [*include_paths(), os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]:
@@ -50,8 +57,8 @@ def build_tensors(force: bool = False) -> str:
     for path in library_paths():
         cmd += ["-L", path]
     subprocess.check_call(cmd + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python"])
-    os.replace(tmp, TENSORS)
-    return TENSORS
+    os.replace(tmp, target)
+    return target
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
