@@ -342,7 +342,7 @@ int spd_batch_step(spd_ctx *const *ctxs, int32_t n, int32_t *out_ids, int32_t *o
  * allocates, and may be captured.  Element types: SPD_F32, SPD_BF16.  Sums, softmax statistics and scores are float32 or wider.
  *
  * What only the device knows (positions, page numbers, parents) is checked there: an entry outside its range is
- * skipped, reads nothing and writes nothing, and *status (DEVICE int32, may be NULL) becomes SPD_ERANGE; it is never set back.
+ * skipped, and what depends on it is neither read nor written; *status (DEVICE int32, may be NULL) becomes SPD_ERANGE; it is never set back.
  *
  * A cache is an array [slots][n_kv_heads][head_dim] for keys and one for values.  A table row lists the pages of a
  * sequence: place i of the sequence is slot table[row][i / page] * page + i % page.  Tables of different page sizes may
@@ -356,7 +356,9 @@ enum { SPD_F32 = 0, SPD_BF16 = 1 };
  * positions on the way: pair p of a head, (x0, x1), becomes (x0 c - x1 s, x0 s + x1 c) with (c, s) = rope[pos][p], float32,
  * rounded once to the type stored (nearest even).  pairs = 0: dimensions 2p and 2p + 1 (the decoder of spd_config);
  * 1: p and p + rot_dim / 2.  Token i goes to place index[i] (NULL: pos[i]) of table row seq[i] (NULL: i), or, when
- * table is NULL, to slot index[i].  A negative index stores nothing (padding); its query is rotated all the same.
+ * table is NULL, to slot index[i].  A negative index stores nothing (padding); its query is rotated all the same.  A position outside `rope`
+ * has no angle: the token's query and key are not written (q_out and the key's slot keep what they held), its value, which needs none, is
+ * stored; *status says so, but for padding, which may hold any position.
  * q / q_out: rotated queries, may be the same array; q NULL leaves them out.  k and v NULL: queries only.  Two tokens
  * of one call must not share a slot.  head_dim a multiple of 8, at most 256; rot_dim a multiple of 8, 0 .. head_dim;
  * rope [rope_rows][rot_dim / 2][2] float32, 16-byte aligned.  kv_dtype: the cache's type, x_dtype: that of q, k, v and q_out.

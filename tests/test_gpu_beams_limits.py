@@ -225,3 +225,26 @@ def test_select_at_a_temperature_near_zero():
     token, parent, new, _, _ = P.spd_beam_select(z, score, tau=1e-39)
     assert list(zip(parent[0].tolist(), token[0].tolist())) == [(0, 7), (0, 4000), (1, 55)]
     assert (new[0].double() - torch.tensor([-1 - math.log(2), -1 - math.log(2), -2.0], device=DEV)).abs().max() <= 2.0 ** -23 * 18
+
+
+# ---------------------------------------------------------------- append: positions without an angle
+@pytest.mark.parametrize("pairs", ["adjacent", "halves"])
+def test_positions_outside_the_angles_write_no_query_and_no_key(pairs):
+    g = gen(31)
+    n, h, d = 4, 2, 64
+    q, k, v = normal(g, n, h, d), normal(g, n, h, d), normal(g, n, h, d)
+    rope = P.spd_rope_table(8, d, device=DEV)
+    for index, bad, told in (([3, 1, 0, 2], 2, -3), ([3, 1, -1, 2], 2, 0)):          # a token that is stored; padding
+        for place in (8, -1, 2 ** 31 - 1, -2 ** 31):
+            pos = [5, 7, 0, 1]
+            pos[bad] = place
+            kc, vc, out = torch.full((4, h, d), 7.0, device=DEV), torch.full((4, h, d), 7.0, device=DEV), torch.full((n, h, d), 7.0, device=DEV)
+            status = torch.zeros(1, dtype=torch.int32, device=DEV)
+            P.spd_cache_append(k, v, kc, vc, i32(pos), rope, q=q, q_out=out, index=i32(index), pairs=pairs, status=status)
+            assert int(status) == told
+            assert (out[bad] == 7).all() and (kc[0] == 7).all()
+            assert torch.equal(vc[0], v[bad]) if told else (vc[0] == 7).all()
+            pos[bad] = 0
+            want = P.spd_cache_append(k, v, kc.clone(), vc.clone(), i32(pos), rope, q=q, index=i32(index), pairs=pairs)
+            rest = [i for i in range(n) if i != bad]
+            assert torch.equal(out[rest], want[rest]) and torch.equal(vc[[3, 1, 2]], v[rest]) and (kc[1:] != 7).any()
