@@ -386,8 +386,10 @@ int spd_cache_append(const spd_append_args *args);
  * its own positions 0 .. own_len[s] - (c - 1 - i) - 1: the queries are the sequence's last c tokens, their keys already
  * in the cache.  out = sum(e^(scale q.k - m) v) / sum(e^(scale q.k - m)) over both; lse (may be NULL) [n][n_heads] float32 = log
  * of the sum of e^(scale q.k).  A row that sees nothing, or nothing but scores of minus infinity, gives zeros and
- * minus infinity; keys and values that a row does not see have no part in it, whatever they hold; those that it sees have to be
- * finite (with float32 queries an infinite one gives NaN).  n_heads is a multiple of n_kv_heads:
+ * minus infinity; keys and values that a row does not see have no part in it, whatever they hold.  Those that it sees have to be
+ * finite (an infinite one gives NaN), over a float32 cache also below 2^128 - 2^116, and so the queries (operands are rounded to their
+ * leading bits, which there is past float32: its largest and lowest numbers give NaN); the sums, taken before the division, must not
+ * pass float32.  n_heads is a multiple of n_kv_heads:
  * query heads h * r .. h * r + r - 1 read key head h.  g = 0: no prefixes.
  * A group's prefix is read once for all its queries (tiles of up to 64 rows share a read), split over its length.
  * scale > 0 and finite.  Types: (x, kv) = (bf16, bf16), (f32, bf16), (f32, f32); out has x's.  The softmax weights enter the second product with 2^-16 of

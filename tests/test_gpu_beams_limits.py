@@ -248,3 +248,26 @@ def test_positions_outside_the_angles_write_no_query_and_no_key(pairs):
             want = P.spd_cache_append(k, v, kc.clone(), vc.clone(), i32(pos), rope, q=q, index=i32(index), pairs=pairs)
             rest = [i for i in range(n) if i != bad]
             assert torch.equal(out[rest], want[rest]) and torch.equal(vc[[3, 1, 2]], v[rest]) and (kc[1:] != 7).any()
+
+
+# ---------------------------------------------------------------- attention: operands of any size that is said to be taken
+@pytest.mark.parametrize("x,kv", [(BF16, BF16), (F32, BF16), (F32, F32)])
+@pytest.mark.parametrize("rows", [1, 20])
+def test_values_and_keys_up_to_the_largest(x, kv, rows):
+    """Values just below the largest that are taken, whose weighted sum stays inside float32; keys whose scores do with small queries."""
+    g = gen(rows)
+    h, d, own = 2, 64, 40
+    largest = 2.0 ** 128 - 2.0 ** 120 if kv == BF16 else 2.0 ** 128 - 2.0 ** 117
+    kc, vc = normal(g, own, h, d).to(kv), normal(g, own, h, d).to(kv)
+    q = normal(g, rows, h, d).to(x)
+    kc[7] = q[0] * -3
+    vc[7, :, :3], vc[7, :, 3:] = largest / 64, 1.0          # 40 weights of 1 at most: the sum stays inside
+    kc[9, :, 0], kc[9, :, 1:] = -largest, 0.0
+    q[:, :, 1:] *= 2.0 ** -4
+    q[:, :, 0] = 2.0 ** -126
+    out, lse = P.spd_shared_attention(q, kc, vc, torch.arange(own, device=DEV).to(torch.int32).expand(rows, own).contiguous(), i32([own] * rows), return_lse=True)
+    s = torch.einsum("nhd,phd->nhp", q.double(), kc.double()) * d ** -0.5
+    want = torch.einsum("nhp,phd->nhd", torch.softmax(s, -1), vc.double())
+    assert out.isfinite().all() and lse.isfinite().all()
+    assert ((out.double() - want).abs() <= want.abs() * (2.0 ** -8 if x == BF16 else 2.0 ** -18) + 2.0 ** -16).all()
+    assert ((lse.double() - torch.logsumexp(s, -1)).abs() <= 2.0 ** -18).all()
