@@ -394,7 +394,7 @@ int spd_cache_append(const spd_append_args *args);
  * A group's prefix is read once for all its queries (tiles of up to 64 rows share a read), split over its length.
  * scale > 0 and finite.  Types: (x, kv) = (bf16, bf16), (f32, bf16), (f32, f32); out has x's.  The softmax weights enter the second product with 2^-16 of
  * their value or better for bf16 queries, 2^-22 for float32 ones; their sum is taken in float32.  head_dim a multiple of 8 (of 4 for a float32
- * cache), at most 256; cache rows of a head start on 16 bytes.  b <= 4096, n <= 2^24, slots < 2^31 (else SPD_ERANGE).  workspace: spd_shared_attention_bytes of DEVICE memory,
+ * cache), at most 256; cache rows of a head start on 16 bytes, the caches' strides are not negative.  b <= 4096, n <= 2^24, slots < 2^31 (else SPD_ERANGE).  workspace: spd_shared_attention_bytes of DEVICE memory,
  * 256-byte aligned, not shared by calls that overlap; the counts n, b, g, heads and head_dim, the types of `args` and whether q_start is
  * set are all that function reads (set is the larger need).  Calls with the same heads, head_dim and types and as many rows,
  * sequences and prefixes or fewer need no more.

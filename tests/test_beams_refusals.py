@@ -4,7 +4,7 @@ import sysconfig
 
 import torch
 
-from tests.test_beams_host import A8, A8L, AT, EINVAL, Reorder, Select, lib, refused   # noqa: F401
+from tests.test_beams_host import A8, A8L, AT, EINVAL, Attention, Reorder, Select, lib, refused   # noqa: F401
 
 
 def test_states_that_lie_on_one_another_are_refused(lib):   # noqa: F811
@@ -31,3 +31,13 @@ def test_each_python_and_torch_has_a_tensor_module_of_its_own(monkeypatch):
     assert beams.load_tensors().__file__ == path and torch.__version__ in path and sysconfig.get_config_var("SOABI") in path
     monkeypatch.setattr(torch, "__version__", "9.9.9")
     assert build.tensors_path() != path and build._stale(build.tensors_path())
+
+
+ATTENTION = dict(q=AT, k_cache=AT, v_cache=AT, out=AT, prefix_table=AT, prefix_len=AT, own_table=AT, own_len=AT, workspace=AT, workspace_bytes=1 << 40,
+                 n=3, b=3, g=1, n_heads=8, n_kv_heads=2, head_dim=64, x_dtype=0, kv_dtype=1, prefix_page=16, prefix_cols=4, own_page=1, own_cols=9, scale=0.125,
+                 kc_slot=128, kc_head=64, vc_slot=128, vc_head=64, slots=100)
+
+
+def test_caches_that_run_backwards_are_refused(lib):   # noqa: F811
+    """Their offsets would have read as places that hold nothing."""
+    refused(lib, "spd_shared_attention", Attention, ATTENTION, [(EINVAL, dict([(name, -128)])) for name in ("kc_slot", "kc_head", "vc_slot", "vc_head")])
