@@ -338,7 +338,7 @@ int spd_batch_step(spd_ctx *const *ctxs, int32_t n, int32_t *out_ids, int32_t *o
  * Operators of k real drafts behind one prompt (what Superposed Decoding is compared with, Section 4.3: k sequences,
  * each with an inference pass of its own per timestep; and beam search over them).  They stand beside the contexts:
  * no context, no weights, all arrays DEVICE memory of the caller, which may be views with strides (in elements, the
- * last dimension contiguous).  Each call enqueues its launches on `stream` and returns; it neither synchronises nor
+ * last dimension contiguous) and lie on whole elements.  Each call enqueues its launches on `stream` and returns; it neither synchronises nor
  * allocates, and may be captured.  Element types: SPD_F32, SPD_BF16.  Sums, softmax statistics and scores are float32 or wider.
  *
  * What only the device knows (positions, page numbers, parents) is checked there: an entry outside its range is

@@ -189,6 +189,8 @@ extern "C" int spd_cache_append(const spd_append_args *args) {
   if (a.q && (!a.q_out || a.n_heads < 1)) return SPD_EINVAL;
   if (a.rot_dim && (!a.rope || !a.pos || a.rope_rows < 1 || !aligned(a.rope, 16))) return SPD_EINVAL;
   if (kv && a.table && (a.page < 1 || a.table_rows < 1 || a.table_cols < 1)) return SPD_EINVAL;
+  if (!all_aligned(type_bytes(a.x_dtype), {a.q, a.k, a.v, a.q_out}) || !all_aligned(type_bytes(a.kv_dtype), {a.k_cache, a.v_cache})) return SPD_EINVAL;
+  if (!all_aligned(4, {a.pos, a.index, a.seq, a.table, a.status})) return SPD_EINVAL;
   if (a.n_heads > 1 << 16 || a.n_kv_heads > 1 << 16) return SPD_ERANGE;
   Append p;
   p.a = a;

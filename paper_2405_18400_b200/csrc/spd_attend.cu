@@ -126,6 +126,7 @@ extern "C" int spd_shared_attention(const spd_attention_args *args) {
   const size_t kv = type_bytes(a.kv_dtype), x = type_bytes(a.x_dtype);
   if (!a.q || !a.k_cache || !a.v_cache || !a.out || !a.own_len || !a.workspace || !aligned(a.workspace, 256) || a.slots < 1) return SPD_EINVAL;
   if (!aligned(a.q, x) || !aligned(a.out, x) || !aligned(a.k_cache, 16) || !aligned(a.v_cache, 16)) return SPD_EINVAL;
+  if (!all_aligned(4, {a.lse, a.q_start, a.group_start, a.prefix_table, a.prefix_len, a.own_table, a.own_len, a.status})) return SPD_EINVAL;
   // (offsets into the caches are unsigned)
   if ((a.kc_slot | a.kc_head | a.vc_slot | a.vc_head) % (int64_t)(16 / kv) || (a.kc_slot | a.kc_head | a.vc_slot | a.vc_head) < 0) return SPD_EINVAL;
   if (a.own_page < 1 || a.own_cols < 0 || (a.own_cols && !a.own_table) || !(a.scale > 0.f) || std::isinf(a.scale)) return SPD_EINVAL;

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "spd.h"
 
 extern "C" int spd_internal_cuda_fail(cudaError_t e, const char *what);
@@ -11,6 +13,12 @@ extern "C" int spd_internal_cuda_fail(cudaError_t e, const char *what);
 namespace spd {
 
 inline bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+// Whether arrays lie on whole elements of so many bytes (null ones do): the host sees to it, since a device faults on those that do not.
+inline bool all_aligned(size_t a, std::initializer_list<const void *> arrays) {
+  for (const void *p : arrays)
+    if (!aligned(p, a)) return false;
+  return true;
+}
 inline size_t type_bytes(int dtype) { return dtype == SPD_F32 ? 4 : 2; }
 inline bool known_type(int dtype) { return dtype == SPD_F32 || dtype == SPD_BF16; }
 inline int launched(const char *what) {

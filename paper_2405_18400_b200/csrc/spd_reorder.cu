@@ -78,7 +78,7 @@ extern "C" int spd_beam_reorder(const spd_reorder_args *args) {
   if (a.n_states < 0 || a.n_states > SPD_MAX_STATES || a.requests < 0 || a.beams < 1) return SPD_EINVAL;
   if (a.beams > 32) return SPD_ERANGE;
   if (a.requests == 0) return SPD_OK;
-  if (!a.parent) return SPD_EINVAL;
+  if (!a.parent || !all_aligned(4, {a.parent, a.status})) return SPD_EINVAL;
   Reorder p;
   p.parent = a.parent;
   p.status = a.status;

@@ -539,6 +539,7 @@ extern "C" int spd_beam_select(const spd_select_args *args) {
   if (a.requests == 0) return SPD_OK;
   if (!a.logits || !a.score || !a.new_token || !a.new_parent || !a.new_score || !a.workspace || !aligned(a.workspace, 256)) return SPD_EINVAL;
   if (!(a.tau > 0.f) || !(a.alpha >= 0.f) || std::isinf(a.alpha) || a.eos_id < -1 || a.eos_id >= a.vocab || !aligned(a.logits, type_bytes(a.x_dtype))) return SPD_EINVAL;
+  if (!all_aligned(4, {a.score, a.length, a.new_token, a.new_parent, a.new_score, a.new_length})) return SPD_EINVAL;
   const SelectPlan l = select_plan(a, aligned(a.logits, 16) && (a.request_stride | a.beam_stride) % (16 / (int64_t)type_bytes(a.x_dtype)) == 0);
   if (a.workspace_bytes < (int64_t)l.bytes) return SPD_ENOMEM;
   Select p;

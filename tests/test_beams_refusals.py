@@ -4,7 +4,7 @@ import sysconfig
 
 import torch
 
-from tests.test_beams_host import A8, A8L, AT, EINVAL, Attention, Reorder, Select, lib, refused   # noqa: F401
+from tests.test_beams_host import A8, A8L, AT, EINVAL, Append, Attention, Reorder, Select, lib, refused   # noqa: F401
 
 
 def test_states_that_lie_on_one_another_are_refused(lib):   # noqa: F811
@@ -41,3 +41,20 @@ ATTENTION = dict(q=AT, k_cache=AT, v_cache=AT, out=AT, prefix_table=AT, prefix_l
 def test_caches_that_run_backwards_are_refused(lib):   # noqa: F811
     """Their offsets would have read as places that hold nothing."""
     refused(lib, "spd_shared_attention", Attention, ATTENTION, [(EINVAL, dict([(name, -128)])) for name in ("kc_slot", "kc_head", "vc_slot", "vc_head")])
+
+
+def test_arrays_that_do_not_lie_on_whole_elements_are_refused(lib):   # noqa: F811
+    append = dict(q=AT, k=AT, v=AT, q_out=AT, k_cache=AT, v_cache=AT, rope=AT, pos=AT, index=AT, seq=AT, table=AT, status=AT, n=3, n_heads=4, n_kv_heads=2,
+                  head_dim=64, rot_dim=64, x_dtype=0, kv_dtype=1, slots=10, page=1, rope_rows=8, table_rows=1, table_cols=1)
+    refused(lib, "spd_cache_append", Append, append, [(EINVAL, dict([(name, AT + 2)])) for name in "q k v q_out rope pos index seq table status".split()])
+    refused(lib, "spd_cache_append", Append, append, [(EINVAL, dict([(name, AT + 1)])) for name in "k_cache v_cache".split()])
+    attention = dict(ATTENTION, lse=AT, q_start=AT, group_start=AT, status=AT)
+    refused(lib, "spd_shared_attention", Attention, attention, [(EINVAL, dict([(name, AT + 2)])) for name in
+            "q out k_cache v_cache lse q_start group_start prefix_table prefix_len own_table own_len status workspace".split()])
+    select = dict(logits=AT, score=AT, length=AT, new_token=AT, new_parent=AT, new_score=AT, new_length=AT, workspace=AT, workspace_bytes=1 << 40, requests=2, beams=4,
+                  vocab=100, x_dtype=0, eos_id=-1, tau=1.0, request_stride=400, beam_stride=100)
+    refused(lib, "spd_beam_select", Select, select, [(EINVAL, dict([(name, AT + 2)])) for name in
+            "logits score length new_token new_parent new_score new_length workspace".split()])
+    reorder = dict(state=A8(*[AT] * 8), outer=A8L(*[1] * 8), outer_stride=A8L(*[64] * 8), request_stride=A8L(*[64] * 8), beam_stride=A8L(*[16] * 8),
+                   row_bytes=A8L(*[16] * 8), parent=AT, status=AT, n_states=1, requests=2, beams=4)
+    refused(lib, "spd_beam_reorder", Reorder, reorder, [(EINVAL, dict(parent=AT + 2)), (EINVAL, dict(status=AT + 1))])
