@@ -59,7 +59,7 @@ def spd_cache_append(k: Optional[torch.Tensor], v: Optional[torch.Tensor], k_cac
     `pos` [n] in `rope` (spd_rope_table; None: no rotation).  Token i goes to place index[i] (default pos[i]) of row seq[i]
     (default i) of `table` [sequences, pages], or to slot index[i] without a table.  Returns the rotated queries (a new tensor, or
     q_out), None without q."""
-    return (_tensors or load_tensors()).cache_append(k, v, k_cache, v_cache, pos, rope, q, q_out, index, seq, table, page, _PAIRS[pairs], status)
+    return (_tensors or load_tensors()).cache_append(k, v, k_cache, v_cache, pos, rope, q, q_out, index, seq, table, page, _PAIRS.get(pairs, -1), status)
 
 
 def spd_shared_attention_workspace(q: torch.Tensor, k_cache: torch.Tensor, own_table: torch.Tensor,

@@ -271,3 +271,8 @@ def test_values_and_keys_up_to_the_largest(x, kv, rows):
     assert out.isfinite().all() and lse.isfinite().all()
     assert ((out.double() - want).abs() <= want.abs() * (2.0 ** -8 if x == BF16 else 2.0 ** -18) + 2.0 ** -16).all()
     assert ((lse.double() - torch.logsumexp(s, -1)).abs() <= 2.0 ** -18).all()
+
+
+def test_pairs_that_are_not_known_are_refused():
+    with pytest.raises(P.SpdError):
+        P.spd_cache_append(None, None, None, None, i32([0]), P.spd_rope_table(2, 8, device=DEV), q=torch.zeros(1, 1, 8, device=DEV), pairs="neither")
