@@ -100,22 +100,21 @@ __device__ __forceinline__ int tiles_of(int rows, int height) { return rows > 0 
 __device__ __forceinline__ int prefix_length(const Attend &p, int g) { return within(p.a.prefix_len[g], p.prefix_room); }
 __device__ __forceinline__ int own_length(const Attend &p, int s) { return within(p.a.own_len[s], p.own_room); }
 
+// (No early return: the lengths are asked for together with the segments' ends.)
 template <int HEIGHT, int STEP>
 __device__ __forceinline__ Cost prefix_cost(const Attend &p, int g) {
   const int first = first_seq(p, g), end = first_seq(p, g + 1);
-  if (end < first) return {-1, 0};
   const int steps = (int)(((unsigned)prefix_length(p, g) + STEP - 1) / STEP);
   const int rows = (first_row(p, end) - first_row(p, first)) * p.ratio;
   const int tiles = steps ? tiles_of(rows, HEIGHT) * p.a.n_kv_heads : 0;
-  return {tiles * steps, tiles};
+  return {end < first ? -1 : tiles * steps, tiles};
 }
 template <int STEP, int HEIGHT>
 __device__ __forceinline__ Cost own_cost(const Attend &p, int s) {
   const int steps = (int)(((unsigned)own_length(p, s) + STEP - 1) / STEP);
   const int rows = (first_row(p, s + 1) - first_row(p, s)) * p.ratio;
-  if (rows < 0) return {-1, 0};
   const int tiles = steps ? tiles_of(rows, HEIGHT) * p.a.n_kv_heads : 0;
-  return {tiles * steps, tiles};
+  return {rows < 0 ? -1 : tiles * steps, tiles};
 }
 
 template <typename F>
@@ -1129,13 +1128,12 @@ struct Attending {
     // the place of the next step to be looked up
     Place place = find_segment(a.b, at, cost);
     int token0 = 0, count = 0, len = 0, steps = 0, high = 0, tiles = 0;
-    int n = end - at;
-    int ahead = 0;               // steps looked up
     const auto enter = [&]() {   // the segment's numbers; empty ones are passed over
 #pragma unroll 1
       for (;;) {
-        if (place.segment >= a.b) {   // (only if the arrays change under the kernel: the run ends)
-          n = ahead, steps = high = 1;
+        if (place.segment >= a.b) {   // (only if the arrays change under the kernel: one tile of no rows and no positions to the run's end)
+          token0 = count = 0, len = -0x7fffffff, steps = 0x7fffffff, high = tiles = 1;
+          place.before = at, place.segment = a.b - 1;
           return;
         }
         token0 = first_row(p, place.segment);
@@ -1152,6 +1150,8 @@ struct Attending {
     };
     enter();
     int tile = (at - place.before) / steps, step = at - place.before - tile * steps, h = tile / high, row = tile - h * high;
+    const int n = end - at;
+    int ahead = 0;               // steps looked up
     int number = -1;
     const auto entry = [&]() {
       const int pos = step * kP + lane;
