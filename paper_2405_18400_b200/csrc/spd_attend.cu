@@ -9,7 +9,8 @@ namespace {
 int mode_of(const spd_attention_args &a) {
   // Tiles of four or eight float32 rows where the mean group (without prefixes: sequence) has no more (larger groups among them have several, and
   // read their prefix as often).  Against tiles of 16, bf16 cache: 3 rows behind 2048 positions 14.6 and 17.3 us, 8 x 3 rows 51 and 66, 4 x 8 rows 37.5 and 42;
-  // float32 cache: 3 rows 22 and 29, 2 x 7 rows behind 8000 positions of 8 key heads 35 and 44.  (256 dimensions of eight rows leave no registers.)
+  // float32 cache: 3 rows 22 and 29, 2 x 7 rows behind 8000 positions of 8 key heads 35 and 44.  Uneven groups gain as well: one of 64 rows
+  // beside 63 of one, 8 key heads, 2048 positions each, 93 and 113 us, float32 cache 200 and 282.  (256 dimensions of eight rows leave no registers.)
   const long long rows = (long long)a.n * (a.n_heads / a.n_kv_heads), groups = a.g ? a.g : a.b;
   if (a.x_dtype == SPD_BF16 && a.kv_dtype == SPD_BF16) return kAttBf16;
   if (a.x_dtype == SPD_F32 && a.kv_dtype == SPD_BF16) return rows <= 4 * groups ? kAttFew : rows <= 8 * groups && a.head_dim <= 128 ? kAttEight : kAttTerms;
@@ -70,8 +71,8 @@ int attend_plan(const spd_attention_args &a, int mode, AttendPlan *l) {
   const long long ratio = a.n_heads / a.n_kv_heads, rows = a.n * ratio;
   // The height of a tile (16, 32 or 64 rows of the mean group): what needs the least time if the blocks take equal runs of the tiles' steps, each
   // step at its measured cost (us of a block among others, 128 dimensions).  Higher tiles read a prefix less often and use operands more often,
-  // lower ones make more runs: 80 float32 rows behind 490 positions of 2 key heads 26 us at 64 rows, 14 at 16; 64 rows behind 4 x 4096 positions of
-  // 32 heads (bf16) 84 us at 64, 130 at 16.  The lengths are the device's, so the tables' room stands for them.
+  // lower ones make more runs: 80 float32 rows behind 490 positions of 2 key heads 26 us at 64 rows, 14 at 16; 64 rows behind each of 4 x 4096
+  // positions of 32 heads (bf16) 130 us at 64, 196 at 16.  The lengths are the device's, so the tables' room stands for them.
   const long long mean = a.g ? (rows + a.g - 1) / a.g : 0, step = (a.kv_dtype == SPD_F32 ? kPositions<kAttFloat> : kPositions<kAttBf16>) * warps;
   const double steps = std::ceil((double)a.prefix_cols * a.prefix_page / step);
   l->rt = 1;

@@ -1,4 +1,4 @@
-// Attention for sequences that share prefixes (Flash-style: one pass over keys and values with the running maximum and sum of
+// Attention for sequences that share prefixes (one pass over keys and values with the running maximum and sum of
 // the softmax), in two launches: partial results of pieces of the positions, then their join per row.
 //
 // Mathematics.  A piece of the positions gives a row (m, l, O) = (max s, sum e^(s-m), sum e^(s-m) v); pieces join by
@@ -22,15 +22,16 @@
 //    operand: one instruction does the work of three (up to four rows over a bf16 cache), or two do (up to eight), the rows' sums
 //    being taken once at the end; a lane has one row instead of two, and the registers that are left make a third block per SM.
 //  * One copy of each piece of code: loops that begin before their first step instead of prologues, masks under a branch instead of a
-//    second instance.  Unrolled twice and thrice the paths pushed one another out of the instruction cache (64 requests 54 us, now 44).
+//    second instance.  Unrolled twice and thrice the paths pushed one another out of the instruction cache (64 requests 54 us instead of 44, weights of one term).
 //
-// Measured (B200, 128 dimensions, lengths as in perf/operators.py): 4 x 8 beams behind 16384 positions of 8 key heads, bf16, 59 us for 277 MB (4.7 TB/s of the
-// copy's 6.46); 8 rows behind 4 x 4096 positions of 32 heads 50 us for 268 MB; 64 requests behind 2048 positions with 50 to 200 of their own 44 us for 165 MB;
+// Measured (B200, 128 dimensions, lengths as in perf/operators.py): 4 x 8 beams behind 16384 positions of 8 key heads, bf16, 68 us for 277 MB (4.1 TB/s of the
+// copy's 6.46); 8 rows behind 4 x 4096 positions of 32 heads 50 us for 268 MB; 64 requests behind 2048 positions with 50 to 200 of their own 48 us for 165 MB;
 // three float32 rows behind 2048 positions 14.6 us for 34 MB, eight times as many 51 for 266; 31 float32 rows over 1001 positions of a float32 cache, 40 heads, 33 us for 52 MB.
 //
 // Roundings.  bf16 queries and cache: products exact, sums float32, the softmax weights e^(s-m) <= 1 as two bf16 terms (the first by truncation, exact; the
 // second to 2^-16 of the weight), so that the output's own rounding is all that shows (error 1.66e-3, as float32 arithmetic rounded once; with weights
-// of one term, 2^-9 each, it was 2.21e-3.  The second term's products cost 64 requests 4 us of 53 and four long prompts 2 of 74, caches cold.)  float32 queries with a
+// of one term, 2^-9 each, it was 2.21e-3.  The second term's products are
+// half as many again behind the softmax: 64 requests 44 -> 48 us, four long prompts 59 -> 68, 64 rows behind each of 4 x 4096 positions of 32 heads 107 -> 130.)  float32 queries with a
 // bf16 cache: queries and weights as three exact bf16 terms.  float32 cache: both sides of both products as two tf32 terms (11 + 11
 // bits), three products.
 #pragma once
@@ -187,7 +188,7 @@ __device__ __forceinline__ Split split_blocks(int blocks, int warps, const Weigh
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(part) : "f"(__fadd_rn(__fmul_rn(wp, warps), wo)));
   int n = pre.steps ? __float2int_rn(__fmul_rn(blocks, __fmul_rn(__fmul_rn(wp, warps), part))) : 0;
   // As many runs for a tile as for another, where that costs no more than a sixth of the blocks: a block that crosses into a second tile
-  // fills its ring anew and writes a second part (four prompts of 8 key heads on 294 blocks 65 us, on 288 60).
+  // fills its ring anew and writes a second part (four prompts of 8 key heads on 294 blocks 65 us, on 288 60, weights of one term).
   if (n > pre.tiles && pre.tiles > 0) {
     const int even = n / pre.tiles * pre.tiles;
     if (n - even <= n / 6) n = even;
